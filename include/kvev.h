@@ -286,6 +286,138 @@ int kvev_compact_attention(const kvev_shape *shape, const void *Q, int Tq, const
  * KVEV_OP_GATED_ATTENTION every T up to T_cap: a growing cache needs one query. */
 size_t kvev_workspace_bytes(int op, const kvev_shape *shape, int n, int k_cap);
 
+/* ---- the paged cache in 4 bits ---------------------------------------------------
+ * Keys and values of many batch rows of different lengths in one pool of pages.
+ * A page holds `page` consecutive tokens of one batch row, for every layer and
+ * key-value head; row b's token t sits in page table[b][t / page].  Elements are held
+ * in blocks of 32 along d: 4-bit floats (sign, two bits of exponent, one of mantissa:
+ * 0, .5, 1, 1.5, 2, 3, 4, 6) times a power of two per block, d + d / 16 bytes per
+ * token and head for key and value together.  The power is the smallest with which the
+ * block's largest magnitude rounds to 6 at most, from 2^-125 to 2^125 (magnitudes above
+ * 7 * 2^125 become 6 * 2^125); elements are rounded to nearest, ties to even, so each is off
+ * by half a step of its code at most.  A block with a value that is not finite reads as
+ * NaN.  Every value held is exact in bf16.
+ *   pool    kvev_page_pool_bytes() bytes, 16-byte aligned; its layout is the library's:
+ *           rows go in and out through kvev_page_append and kvev_page_read
+ *   table   [B, max_pages] int32: page of the pool, or -1: none
+ *   length  [B] int32: tokens that the row holds
+ *   refs    [n_pages] int32: table entries that name the page; 0: free.  There is
+ *           nothing else to know of a page, and pages are handed out lowest index first.
+ * A fresh cache is table = -1, length = 0, refs = 0, whatever the pool holds.
+ * Of `shape`, L, B, H, H_kv, d and dtype (the type of Q, K, V, O and summaries) are used,
+ * and T by kvev_page_attention.  The int32 arrays are 4-byte aligned device pointers.
+ * Entries of device arrays are not checked on the host.  The kernels keep to the pool
+ * whatever they hold: a table entry outside [0, n_pages) is no page, lengths are cut to
+ * [0, max_pages * page].  Calls that write the same arrays must not overlap in time.
+ * `status`: one int32 in device memory into which calls or the bits KVEV_PAGES_*; the
+ * library never clears it.
+ * Supported: page in {16, 32, 64, 128, 256}; max_pages * page < 2^31 - 256,
+ * B * (max_pages + 1) and L * n_pages < 2^31. */
+typedef struct {
+    int32_t page, n_pages, max_pages;
+} kvev_pages;
+enum { KVEV_PAGES_NONE_FREE = 1,      /* not enough free pages (reserve), or pages of the target (compact) */
+       KVEV_PAGES_BAD_ROW = 2,        /* a row past its capacity, or whose last page is missing (reserve) */
+       KVEV_PAGES_BAD_PAIR = 4 };     /* a pair of fork or copy that was refused */
+enum { KVEV_OP_PAGE_ATTENTION = 16, KVEV_OP_PAGES_RESERVE = 17, KVEV_OP_PAGES_COMPACT = 18 };
+
+size_t kvev_page_pool_bytes(const kvev_shape *shape, const kvev_pages *pages);
+
+/* Scratch bytes of a paged call (0: none, or arguments that are not valid).  n: Tq of
+ * kvev_page_attention, else unused. */
+size_t kvev_page_workspace_bytes(int op, const kvev_shape *shape, const kvev_pages *pages, int n);
+
+/* New rows into the pages: K, V [L,B,H_kv,Tn,d]; row t < n_new[b] of batch row b becomes
+ * token start[b] + t (n_new NULL: all Tn; more than Tn count as Tn).  Nothing is written for
+ * a batch row with start[b] < 0, nor for tokens past the capacity or without a page.  Tokens
+ * that are there may be written again.  No two rows of a call may name the same token of the
+ * same page.  Does not look at lengths: kvev_pages_reserve makes room, moves them on and gives `start`. */
+int kvev_page_append(const kvev_shape *shape, const kvev_pages *pages, const void *K, const void *V, int Tn,
+                     const int32_t *start, const int32_t *n_new, const int32_t *table, void *pool, void *stream);
+
+/* Rows out of the pages, exactly (for kvev_chunk_pool, which takes contiguous rows): token
+ * first[b] + t goes to row t < n[b] of K, V [L,B,H_kv,Tn,d] (n NULL: all Tn); zeros where
+ * there is no page.  Rows from n[b] on are left as they were, and so is everything of a batch
+ * row with first[b] < 0 and what lies past the capacity. */
+int kvev_page_read(const kvev_shape *shape, const kvev_pages *pages, const void *pool, const int32_t *table,
+                   const int32_t *first, const int32_t *n, int Tn, void *K, void *V, void *stream);
+
+/* Eq. 1 over the pages: the queries Q [L,B,H,Tq,d] of batch row b attend, per key-value
+ * head, to rows 0 .. count - 1 of a compact store as kvev_retain leaves it (Kc, Vc
+ * [L,B,H_kv,k_cap,d], count [L,B,H_kv]; k_cap = 0: none, the pointers may be NULL) and to
+ * the tokens [first[b], length[b]) of the pages (first NULL: from 0).  q_start NULL: every
+ * query sees all of them.  Else query i is token q_start[b] + i and sees those up to itself;
+ * with q_start as kvev_pages_reserve gives it, the queries are the tokens just appended.  (In
+ * a padded batch, queries from n_new[b] on get some finite output that means nothing.)  Tokens without a
+ * page are left out.  A query that sees no row gives zeros.
+ * Scores, softmax and sums are fp32, O is rounded once.  fp32: operands enter the matrix
+ * cores as three bf16 terms; bf16: the softmax weights as two, 16 significant bits.  shape->T (0: the capacity) says for what length of row the launch is made; any
+ * length is right, and results depend on it in the order of sums only.
+ * Workspace: kvev_page_workspace_bytes(KVEV_OP_PAGE_ATTENTION, shape, pages, Tq), enough for
+ * every T; zero-filled before its first use, tickets as in kvev_gated_attention.  O must not overlap Q. */
+int kvev_page_attention(const kvev_shape *shape, const kvev_pages *pages, const void *Q, int Tq, const void *pool,
+                        const int32_t *table, const int32_t *length, const int32_t *first, const int32_t *q_start,
+                        const void *Kc, const void *Vc, const int32_t *count, int k_cap, void *O, void *ws,
+                        size_t ws_bytes, void *stream);
+
+/* Room for n_new[b] >= 0 more tokens in every batch row: missing pages are taken, start[b] =
+ * the old length, length[b] += n_new[b].  A row that goes on in a page which others hold as
+ * well gets a copy of it first (of what it has in use).  Free pages go to rows in ascending
+ * order, lowest index first, a row's copy before its new pages.  If there are not enough for all,
+ * nothing changes but start = -1 throughout and KVEV_PAGES_NONE_FREE; a row past its capacity or without its
+ * last page is left alone with start = -1 and KVEV_PAGES_BAD_ROW.  (kvev_page_append skips rows
+ * whose start is -1.)  n_new, length and start are three arrays.  Workspace:
+ * KVEV_OP_PAGES_RESERVE, written by every call. */
+int kvev_pages_reserve(const kvev_shape *shape, const kvev_pages *pages, const int32_t *n_new, int32_t *table,
+                       int32_t *length, int32_t *refs, void *pool, int32_t *start, int32_t *status, void *ws,
+                       size_t ws_bytes, void *stream);
+
+/* Batch row dst[i] (empty: length 0) becomes a second holder of row src[i]'s pages and length,
+ * i < n <= B.  No keys or values move: kvev_pages_reserve copies a shared page when a row writes on in
+ * it.  A pair is refused (KVEV_PAGES_BAD_PAIR, the others go ahead) if a row is outside [0, B),
+ * if dst[i] is not empty or stands in an earlier pair, or if src[i] is some pair's dst. */
+int kvev_pages_fork(const kvev_shape *shape, const kvev_pages *pages, const int32_t *src, const int32_t *dst, int n,
+                    int32_t *table, int32_t *length, int32_t *refs, int32_t *status, void *stream);
+
+/* Batch row rows[i] (NULL: row i), i < n <= B, keeps tokens [first[i], keep[i]) of those it holds
+ * (first NULL: 0, keep NULL: its length): length = min(length, keep), entries of pages wholly
+ * outside become -1, and a page that nobody else holds is free.  keep = 0 gives up the row.  Rows
+ * outside [0, B) are passed over; a row given twice ends with the smaller keep. */
+int kvev_pages_trim(const kvev_shape *shape, const kvev_pages *pages, const int32_t *rows, int n,
+                    const int32_t *first, const int32_t *keep, int32_t *table, int32_t *length, int32_t *refs,
+                    void *stream);
+
+/* Page dst[i] becomes a copy of page src[i], i < n <= n_pages, all layers and heads; tables and
+ * counts are the caller's.  Refused pairs as in kvev_pages_fork (outside [0, n_pages), dst in an
+ * earlier pair, src some pair's dst). */
+int kvev_pages_copy(const kvev_shape *shape, const kvev_pages *pages, void *pool, const int32_t *src,
+                    const int32_t *dst, int n, int32_t *status, void *stream);
+
+/* The pages in use (refs > 0), in ascending order, into the first pages of another pool, which may
+ * be smaller (to->n_pages; to->page and to->max_pages as in `pages`): to_pool, to_table
+ * [B, max_pages] (may be table itself), to_refs [to->n_pages].  Pages of to_pool behind them are left as
+ * they were, their counts are 0.  If there are too few, nothing is written but KVEV_PAGES_NONE_FREE.  The pools and the
+ * counts must not overlap.  Workspace: KVEV_OP_PAGES_COMPACT of the source. */
+int kvev_pages_compact(const kvev_shape *shape, const kvev_pages *pages, const void *pool, const int32_t *table,
+                       const int32_t *refs, const kvev_pages *to, void *to_pool, int32_t *to_table, int32_t *to_refs,
+                       int32_t *status, void *ws, size_t ws_bytes, void *stream);
+
+/* Rotary positions of tokens with up to four coordinates (time, height, width of a frame's image
+ * tokens): pair j < P = sum(section) of a head's elements is turned by pos[a][b][t] * freq[j], a
+ * the axis into whose section j falls (sections lie one after the other):
+ *   y1 = x1 cos - x2 sin,  y2 = x1 sin + x2 cos.
+ * KVEV_ROTARY_HALVES: pair j is elements j and P + j; KVEV_ROTARY_PAIRS: 2 j and 2 j + 1.
+ * Elements from 2 P on are copied.  inverse = 1 turns back, which is also the gradient: with
+ * Q, K the gradients of the outputs, the outputs are those of the inputs.
+ *   Q, Q_out [L,B,H,Tq,d], K, K_out [L,B,H_kv,Tq,d]  (either pair may be NULL; in place: the same
+ *   pointer, else no two may overlap)      freq [P] fp32      pos [n_axes,B,Tq] int32
+ * Angles are taken in 64 bits, products in fp32, each element is rounded once.  Needs
+ * 1 <= P <= d / 2, sections >= 0, L * B * H * Tq <= 2^28. */
+typedef struct { int32_t n_axes, section[4], layout; } kvev_rotary_axes;
+enum { KVEV_ROTARY_HALVES = 0, KVEV_ROTARY_PAIRS = 1 };
+int kvev_rotary(const kvev_shape *shape, const kvev_rotary_axes *axes, const float *freq, const int32_t *pos, int Tq,
+                const void *Q, const void *K, void *Q_out, void *K_out, int inverse, void *stream);
+
 /* Static description of a status code. */
 const char *kvev_status_string(int status);
 

@@ -30,10 +30,15 @@ POOL_MEAN, POOL_MLP, POOL_MAX, POOL_TOKEN_MLP = 0, 1, 2, 3
 SELECT_TOPK, SELECT_THRESHOLD = 0, 1
 OP_CHUNK_POOL, OP_LSTM_GATE, OP_SELECT, OP_GATED_ATTENTION, OP_DENSE_ATTENTION, OP_COMPACT_ATTENTION = range(6)
 OP_LSTM_PREPARE, OP_LSTM_GATE_PREPARED = 6, 7
+OP_PAGE_ATTENTION, OP_PAGES_RESERVE, OP_PAGES_COMPACT = 16, 17, 18
+PAGES_NONE_FREE, PAGES_BAD_ROW, PAGES_BAD_PAIR = 1, 2, 4          # bits of a paged cache's status word
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
 
 EXPORTS = ("kvev_chunk_pool", "kvev_lstm_gate", "kvev_lstm_prepare", "kvev_lstm_gate_prepared", "kvev_select", "kvev_gated_attention",
            "kvev_gated_attention_static", "kvev_dense_attention", "kvev_retain", "kvev_compact_attention", "kvev_workspace_bytes",
-           "kvev_status_string", "kvev_last_hip_error", "kvev_version")
+           "kvev_status_string", "kvev_last_hip_error", "kvev_version",
+           "kvev_page_pool_bytes", "kvev_page_workspace_bytes", "kvev_page_append", "kvev_page_read", "kvev_page_attention",
+           "kvev_pages_reserve", "kvev_pages_fork", "kvev_pages_trim", "kvev_pages_copy", "kvev_pages_compact", "kvev_rotary")
 TEST_HOOKS = ("kvev_debug_pair_wait", "kvev_debug_lstm_fused_min_groups", "kvev_debug_lstm_quad_groups", "kvev_debug_stream_probe",
               "kvev_debug_attn_stream_bytes", "kvev_debug_lstm_plan", "kvev_debug_lstm_form",
               "kvev_debug_pool_form", "kvev_debug_decode_queries")      # include/kvev_test_hooks.h
@@ -42,6 +47,14 @@ TEST_HOOKS = ("kvev_debug_pair_wait", "kvev_debug_lstm_fused_min_groups", "kvev_
 class Shape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("L", "B", "H", "d", "T", "T_cap", "C", "N_cap", "W", "d_sum", "d_g", "dtype", "H_kv")]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("page", "n_pages", "max_pages")]
+
+
+class RotaryAxes(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("section", ctypes.c_int32 * 4), ("layout", ctypes.c_int32)]
 
 
 class MlpW(ctypes.Structure):
@@ -118,14 +131,31 @@ def lib() -> ctypes.CDLL:
         L.kvev_debug_lstm_plan.restype = ci
         L.kvev_debug_stream_probe.argtypes = [vp, sz, ci, vp, sz, ci, ci, vp]
         L.kvev_debug_stream_probe.restype = ci
+        pgp, axp = ctypes.POINTER(Pages), ctypes.POINTER(RotaryAxes)
+        L.kvev_page_pool_bytes.argtypes = [shp, pgp]
+        L.kvev_page_pool_bytes.restype = sz
+        L.kvev_page_workspace_bytes.argtypes = [ci, shp, pgp, ci]
+        L.kvev_page_workspace_bytes.restype = sz
+        L.kvev_page_append.argtypes = [shp, pgp, vp, vp, ci, vp, vp, vp, vp, vp]
+        L.kvev_page_read.argtypes = [shp, pgp, vp, vp, vp, vp, ci, vp, vp, vp]
+        L.kvev_page_attention.argtypes = [shp, pgp, vp, ci, vp, vp, vp, vp, vp, vp, vp, vp, ci, vp, vp, sz, vp]
+        L.kvev_pages_reserve.argtypes = [shp, pgp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.kvev_pages_fork.argtypes = [shp, pgp, vp, vp, ci, vp, vp, vp, vp, vp]
+        L.kvev_pages_trim.argtypes = [shp, pgp, vp, ci, vp, vp, vp, vp, vp, vp]
+        L.kvev_pages_copy.argtypes = [shp, pgp, vp, vp, vp, ci, vp, vp]
+        L.kvev_pages_compact.argtypes = [shp, pgp, vp, vp, vp, pgp, vp, vp, vp, vp, vp, sz, vp]
+        L.kvev_rotary.argtypes = [shp, axp, vp, vp, ci, vp, vp, vp, vp, ci, vp]
         L.kvev_status_string.argtypes = [ci]
         L.kvev_status_string.restype = ctypes.c_char_p
         L.kvev_last_hip_error.restype = ctypes.c_char_p
         for n in ("kvev_chunk_pool", "kvev_lstm_gate", "kvev_lstm_prepare", "kvev_lstm_gate_prepared", "kvev_select", "kvev_gated_attention",
-                  "kvev_gated_attention_static", "kvev_dense_attention", "kvev_retain", "kvev_compact_attention", "kvev_version"):
+                  "kvev_gated_attention_static", "kvev_dense_attention", "kvev_retain", "kvev_compact_attention", "kvev_version",
+                  "kvev_page_append", "kvev_page_read", "kvev_page_attention", "kvev_pages_reserve", "kvev_pages_fork", "kvev_pages_trim",
+                  "kvev_pages_copy", "kvev_pages_compact", "kvev_rotary"):
             getattr(L, n).restype = ci
         _native = _native or _import_native()
         if _native:
+            _native.bind_pages(Pages, RotaryAxes, torch.float32, torch.bfloat16, torch.int32, torch.uint8)
             _native.bind(Shape, RowsFrom, torch.Tensor, torch.cuda.is_initialized, getattr(torch._C, "_cuda_getDevice", None),
                          getattr(torch._C, "_cuda_getCurrentRawStream", None),
                          {n: ctypes.cast(getattr(L, n), vp).value for n in EXPORTS})
@@ -334,6 +364,211 @@ def kvev_compact_attention(shape: Shape, Q, Tq, Kw, Vw, Kc, Vc, count, k_cap, O,
                                           ws.numel() if ws is not None else 0, _stream())
     if st:
         _check(st, "kvev_compact_attention")
+
+
+# ---- the paged 4-bit cache, rotary positions ----
+# What these take is checked here as well as in the library: a tensor's kind of element, its size and its device, which an
+# address does not tell.
+
+def make_pages(page: int, n_pages: int, max_pages: int) -> Pages:
+    return Pages(page, n_pages, max_pages)
+
+
+def make_rotary_axes(sections, layout: int = ROTARY_HALVES) -> RotaryAxes:
+    """Sections (pairs of elements) of up to four coordinates."""
+    n = len(sections)
+    if not 1 <= n <= 4:
+        raise KvevError(ERR_INVALID_ARG, "rotary positions have one to four coordinates")
+    return RotaryAxes(n, (ctypes.c_int32 * 4)(*sections), layout)
+
+
+def page_pool_bytes(shape: Shape, pages: Pages) -> int:
+    return int(lib().kvev_page_pool_bytes(ctypes.byref(shape), ctypes.byref(pages)))
+
+
+def page_workspace_bytes(op: int, shape: Shape, pages: Pages, n: int) -> int:
+    return int(lib().kvev_page_workspace_bytes(op, ctypes.byref(shape), ctypes.byref(pages), n))
+
+
+_STORED = {F32: torch.float32, BF16: torch.bfloat16}
+
+
+def _arg(call, name, t, numel, dtype, optional=False):
+    """The address of a tensor that holds at least `numel` elements of `dtype` on the current device."""
+    if t is None:
+        if optional:
+            return None
+        raise KvevError(ERR_INVALID_ARG, f"{call}: {name} is missing")
+    if t.dtype != dtype or t.numel() < numel:
+        raise KvevError(ERR_INVALID_ARG, f"{call}: {name} has to hold {numel} elements of {dtype}, not {t.numel()} of {t.dtype}")
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise KvevError(ERR_INVALID_ARG, f"{call}: {name} is not on the current device")
+    return _ptr(t)
+
+
+class _Args:
+    """Argument checks of one call."""
+
+    def __init__(self, call: str, shape: Shape, pages: Optional[Pages] = None):
+        self.call, self.shape, self.pages = call, shape, pages
+        self.kv = shape.H_kv or shape.H
+
+    def ints(self, name, t, numel, optional=False):
+        return _arg(self.call, name, t, numel, torch.int32, optional)
+
+    def rows(self, name, t, heads, n, optional=False):
+        s = self.shape
+        return _arg(self.call, name, t, s.L * s.B * heads * n * s.d, _STORED.get(s.dtype), optional)
+
+    def table(self, t, name="table"):
+        return self.ints(name, t, self.shape.B * self.pages.max_pages)
+
+    def pool(self, t, pages=None, name="pool"):
+        return _arg(self.call, name, t, page_pool_bytes(self.shape, pages or self.pages), torch.uint8)
+
+    def scratch(self, t):
+        return (None, 0) if t is None else (_arg(self.call, "ws", t, 0, torch.uint8), t.numel())
+
+
+def kvev_page_append(shape: Shape, pages: Pages, K, V, Tn, start, n_new, table, pool):
+    st = _native.page_append(shape, pages, K, V, Tn, start, n_new, table, pool) if _native else None
+    if st is None:
+        a = _Args("kvev_page_append", shape, pages)
+        st = lib().kvev_page_append(ctypes.byref(shape), ctypes.byref(pages), a.rows("K", K, a.kv, Tn), a.rows("V", V, a.kv, Tn), Tn,
+                                    a.ints("start", start, shape.B), a.ints("n_new", n_new, shape.B, True), a.table(table), a.pool(pool),
+                                    _stream())
+    if st:
+        _check(st, "kvev_page_append")
+
+
+def kvev_page_read(shape: Shape, pages: Pages, pool, table, first, n, Tn, K, V):
+    st = _native.page_read(shape, pages, pool, table, first, n, Tn, K, V) if _native else None
+    if st is None:
+        a = _Args("kvev_page_read", shape, pages)
+        st = lib().kvev_page_read(ctypes.byref(shape), ctypes.byref(pages), a.pool(pool), a.table(table), a.ints("first", first, shape.B),
+                                  a.ints("n", n, shape.B, True), Tn, a.rows("K", K, a.kv, Tn), a.rows("V", V, a.kv, Tn), _stream())
+    if st:
+        _check(st, "kvev_page_read")
+
+
+def kvev_page_attention(shape: Shape, pages: Pages, Q, Tq, pool, table, length, O, ws=None, first=None, q_start=None, Kc=None, Vc=None,
+                        count=None, k_cap=0):
+    st = (_native.page_attention(shape, pages, Q, Tq, pool, table, length, O, ws, first, q_start, Kc, Vc, count, k_cap) if _native
+          else None)
+    if st is None:
+        a, B = _Args("kvev_page_attention", shape, pages), shape.B
+        wp, wn = a.scratch(ws)
+        st = lib().kvev_page_attention(ctypes.byref(shape), ctypes.byref(pages), a.rows("Q", Q, shape.H, Tq), Tq, a.pool(pool), a.table(table),
+                                       a.ints("length", length, B), a.ints("first", first, B, True), a.ints("q_start", q_start, B, True),
+                                       a.rows("Kc", Kc, a.kv, k_cap, k_cap == 0), a.rows("Vc", Vc, a.kv, k_cap, k_cap == 0),
+                                       a.ints("count", count, shape.L * B * a.kv, k_cap == 0), k_cap, a.rows("O", O, shape.H, Tq), wp, wn,
+                                       _stream())
+    if st:
+        _check(st, "kvev_page_attention")
+
+
+def kvev_pages_reserve(shape: Shape, pages: Pages, n_new, table, length, refs, pool, start, status, ws):
+    st = _native.pages_reserve(shape, pages, n_new, table, length, refs, pool, start, status, ws) if _native else None
+    if st is None:
+        a, B = _Args("kvev_pages_reserve", shape, pages), shape.B
+        wp, wn = a.scratch(ws)
+        st = lib().kvev_pages_reserve(ctypes.byref(shape), ctypes.byref(pages), a.ints("n_new", n_new, B), a.table(table),
+                                      a.ints("length", length, B), a.ints("refs", refs, pages.n_pages), a.pool(pool),
+                                      a.ints("start", start, B), a.ints("status", status, 1), wp, wn, _stream())
+    if st:
+        _check(st, "kvev_pages_reserve")
+
+
+def kvev_pages_fork(shape: Shape, pages: Pages, src, dst, n, table, length, refs, status):
+    st = _native.pages_fork(shape, pages, src, dst, n, table, length, refs, status) if _native else None
+    if st is None:
+        a = _Args("kvev_pages_fork", shape, pages)
+        st = lib().kvev_pages_fork(ctypes.byref(shape), ctypes.byref(pages), a.ints("src", src, n), a.ints("dst", dst, n), n, a.table(table),
+                                   a.ints("length", length, shape.B), a.ints("refs", refs, pages.n_pages), a.ints("status", status, 1),
+                                   _stream())
+    if st:
+        _check(st, "kvev_pages_fork")
+
+
+def kvev_pages_trim(shape: Shape, pages: Pages, rows, n, first, keep, table, length, refs):
+    st = _native.pages_trim(shape, pages, rows, n, first, keep, table, length, refs) if _native else None
+    if st is None:
+        a = _Args("kvev_pages_trim", shape, pages)
+        st = lib().kvev_pages_trim(ctypes.byref(shape), ctypes.byref(pages), a.ints("rows", rows, n, True), n, a.ints("first", first, n, True),
+                                   a.ints("keep", keep, n, True), a.table(table), a.ints("length", length, shape.B),
+                                   a.ints("refs", refs, pages.n_pages), _stream())
+    if st:
+        _check(st, "kvev_pages_trim")
+
+
+def kvev_pages_copy(shape: Shape, pages: Pages, pool, src, dst, n, status):
+    a = _Args("kvev_pages_copy", shape, pages)
+    st = lib().kvev_pages_copy(ctypes.byref(shape), ctypes.byref(pages), a.pool(pool), a.ints("src", src, n), a.ints("dst", dst, n), n,
+                               a.ints("status", status, 1), _stream())
+    _check(st, "kvev_pages_copy")
+
+
+def kvev_pages_compact(shape: Shape, pages: Pages, pool, table, refs, to: Pages, to_pool, to_table, to_refs, status, ws):
+    a = _Args("kvev_pages_compact", shape, pages)
+    wp, wn = a.scratch(ws)
+    st = lib().kvev_pages_compact(ctypes.byref(shape), ctypes.byref(pages), a.pool(pool), a.table(table), a.ints("refs", refs, pages.n_pages),
+                                  ctypes.byref(to), a.pool(to_pool, to, "to_pool"), a.table(to_table, "to_table"),
+                                  a.ints("to_refs", to_refs, to.n_pages), a.ints("status", status, 1), wp, wn, _stream())
+    _check(st, "kvev_pages_compact")
+
+
+def kvev_rotary(shape: Shape, axes: RotaryAxes, freq, pos, Tq, Q, K, Q_out, K_out, inverse=0):
+    st = _native.rotary(shape, axes, freq, pos, Tq, Q, K, Q_out, K_out, inverse) if _native else None
+    if st is None:
+        a = _Args("kvev_rotary", shape)
+        pairs = sum(axes.section[:max(0, min(axes.n_axes, 4))])
+        st = lib().kvev_rotary(ctypes.byref(shape), ctypes.byref(axes), _arg(a.call, "freq", freq, pairs, torch.float32),
+                               a.ints("pos", pos, axes.n_axes * shape.B * Tq), Tq, a.rows("Q", Q, shape.H, Tq, True),
+                               a.rows("K", K, a.kv, Tq, True), a.rows("Q_out", Q_out, shape.H, Tq, True),
+                               a.rows("K_out", K_out, a.kv, Tq, True), inverse, _stream())
+    if st:
+        _check(st, "kvev_rotary")
+
+
+class PagedCache:
+    """Caller-owned buffers of one paged 4-bit cache (pool, page table, lengths, holders of each page, scratch).
+    Allocation only; no arithmetic."""
+
+    def __init__(self, shape: Shape, page: int, n_pages: int, max_pages: int, Tq: int = 1, device="cuda"):
+        self.shape, self.pages = shape, make_pages(page, n_pages, max_pages)
+        nbytes = page_pool_bytes(shape, self.pages)
+        if nbytes == 0:
+            raise KvevError(ERR_INVALID_ARG, f"no such cache: pages of {page} tokens, {n_pages} of them, {max_pages} to a row")
+
+        def ints(*size, fill=0):
+            return torch.full(size, fill, dtype=torch.int32, device=device)
+        self.pool = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.table, self.length, self.refs = ints(shape.B, max_pages, fill=-1), ints(shape.B), ints(n_pages)
+        self.start, self.status = ints(shape.B), ints(1)
+        self.ws = alloc_workspace(page_workspace_bytes(OP_PAGES_RESERVE, shape, self.pages, 0), device)
+        # (the attention's own: its tickets must stay zero between calls)
+        self.ws_attn = alloc_workspace(page_workspace_bytes(OP_PAGE_ATTENTION, shape, self.pages, Tq), device)
+
+    def reserve(self, n_new):
+        kvev_pages_reserve(self.shape, self.pages, n_new, self.table, self.length, self.refs, self.pool, self.start, self.status, self.ws)
+
+    def append(self, K, V, Tn, n_new=None):
+        """The rows for which reserve() last made room."""
+        kvev_page_append(self.shape, self.pages, K, V, Tn, self.start, n_new, self.table, self.pool)
+
+    def attend(self, Q, Tq, O, first=None, causal=False, Kc=None, Vc=None, count=None, k_cap=0):
+        """causal: the queries are the tokens for which reserve() last made room."""
+        kvev_page_attention(self.shape, self.pages, Q, Tq, self.pool, self.table, self.length, O, self.ws_attn, first,
+                            self.start if causal else None, Kc, Vc, count, k_cap)
+
+    def read(self, first, n, Tn, K, V):
+        kvev_page_read(self.shape, self.pages, self.pool, self.table, first, n, Tn, K, V)
+
+    def fork(self, src, dst, n):
+        kvev_pages_fork(self.shape, self.pages, src, dst, n, self.table, self.length, self.refs, self.status)
+
+    def trim(self, rows, n, first=None, keep=None):
+        kvev_pages_trim(self.shape, self.pages, rows, n, first, keep, self.table, self.length, self.refs)
 
 
 class DecodeState:

@@ -11,6 +11,7 @@
 #include <mutex>
 
 #include "../../include/kvev_test_hooks.h"
+#include "api.hpp"
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -18,16 +19,14 @@ namespace kvev {
 
 static thread_local char g_hip_err[256] = "";
 
-static int hip_fail(hipError_t e)
+int hip_fail(hipError_t e)
 {
     snprintf(g_hip_err, sizeof g_hip_err, "%s", hipGetErrorString(e));
     return KVEV_ERR_HIP;
 }
 
-static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 // 0 when the shape itself is usable, else a status.
-static int check_shape(const kvev_shape *sh, bool chunked = true)
+int check_shape(const kvev_shape *sh, bool chunked)
 {
     if (!sh) return KVEV_ERR_INVALID_ARG;
     if (sh->L < 1 || sh->B < 1 || sh->H < 1 || sh->d < 1 || sh->C < 1 || sh->T < 0 || sh->T_cap < 1 ||
@@ -40,9 +39,6 @@ static int check_shape(const kvev_shape *sh, bool chunked = true)
     if (sh->d != 64 && sh->d != 128) return KVEV_ERR_UNSUPPORTED;
     return KVEV_OK;
 }
-
-// key-value heads: the caches, summaries, gate state and kept sets exist per (layer, batch row, KV head)
-static int kv_heads(const kvev_shape *sh) { return sh->H_kv > 0 ? sh->H_kv : sh->H; }
 
 static int n_cand_of(const kvev_shape *sh) { return (sh->T > sh->W ? sh->T - sh->W : 0) / sh->C; }
 
@@ -178,8 +174,6 @@ __global__ __launch_bounds__(256) void fill_zero_kernel(uint4 *p, size_t n16)
     if (i < n16) p[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-static int device_compute_units();
-
 static int attention_common(const kvev_shape *sh, const void *Q, int Tq, const void *K, const void *V,
                             const void *Kbar, const void *Vbar, const int32_t *idx, const int32_t *count,
                             int k_cap, int gated, int causal, void *O, void *ws, size_t ws_bytes,
@@ -254,7 +248,7 @@ static std::atomic<int> g_pair_spin_limit{1 << 22}, g_pair_mute{-1};
 
 // Compute units of the current device (what decides whether the workgroups of a paired launch can all be resident);
 // 256 when no device answers (argument checks and scratch queries also run on machines without a GPU).
-static int device_compute_units()
+int device_compute_units()
 {
     static std::atomic<int> cached{0};
     int n = cached.load();

@@ -1,0 +1,291 @@
+// C-ABI layer of the paged 4-bit cache and of rotary positions: argument validation (host only, before any HIP call), launch
+// planning, dispatch.
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "api.hpp"
+#include "kernels.hpp"
+#include "pages.hpp"
+
+namespace kvev {
+
+static bool aligned4(const void *p) { return p && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+static bool aligned4_or_null(const void *p) { return !p || aligned4(p); }
+static bool whole16(const void *p) { return p && aligned16(p); }
+
+// whether [p, p + n) and [q, q + m) share a byte
+static bool overlap(const void *p, size_t n, const void *q, size_t m)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
+    return x < y + m && y < x + n;
+}
+
+static int check_pages(const kvev_shape *sh, const kvev_pages *pg, PageGeom *g)
+{
+    const int rc = check_shape(sh, false);
+    if (rc) return rc;
+    if (!pg || pg->n_pages < 1 || pg->max_pages < 1) return KVEV_ERR_INVALID_ARG;
+    int shift = 0;
+    while (shift < 9 && 1 << shift != pg->page) ++shift;
+    if (shift < 4 || shift > 8) return KVEV_ERR_UNSUPPORTED;
+    // positions are 31 bits, and so are the places of table entries and the sums of page counts
+    if (((int64_t)pg->max_pages << shift) > INT32_MAX - 256) return KVEV_ERR_INVALID_ARG;
+    if ((int64_t)sh->B * ((int64_t)pg->max_pages + 1) > INT32_MAX || (int64_t)sh->L * pg->n_pages > INT32_MAX) return KVEV_ERR_INVALID_ARG;
+    *g = PageGeom{sh->L, sh->B, kv_heads(sh), sh->d, shift, pg->n_pages, pg->max_pages};
+    return KVEV_OK;
+}
+static size_t elem(const kvev_shape *sh) { return sh->dtype == KVEV_F32 ? 4 : 2; }
+static size_t pool_bytes(const PageGeom &g) { return (size_t)g.L * g.n_pages * page_bytes(g); }
+
+// ---- attention over pages: planning ----
+// A unit is 16 queries of a key-value head; its rows are shared by up to nsplit workgroups, and a row of the batch takes as many of
+// them as its own length pays for (decided on the device: the lengths are there).  shape->T, or the capacity if it is 0, says for
+// which length nsplit is made; results do not depend on it beyond the order of sums.
+constexpr int kPageChunk = 64, kPageMaxSplit = 64, kPageMinChunks = 4;
+struct PageAttnPlan { int qtiles, nsplit; int64_t units; size_t ticket_bytes, ws_bytes; };
+static PageAttnPlan plan_page_attn(const kvev_shape *sh, const PageGeom &g, int Tq, int64_t tokens)
+{
+    PageAttnPlan p;
+    const int64_t R = (int64_t)(sh->H / g.Hkv) * Tq;
+    p.qtiles = (int)((R + 15) / 16);
+    p.units = (int64_t)g.L * g.B * g.Hkv * p.qtiles;
+    const int64_t chunks = (tokens + kPageChunk - 1) / kPageChunk, target = 4 * (int64_t)device_compute_units();
+    const int64_t want = std::min((target + p.units - 1) / p.units, (chunks + kPageMinChunks - 1) / kPageMinChunks);
+    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(want, kPageMaxSplit));
+    p.ticket_bytes = ((size_t)p.units * sizeof(int32_t) + 255) / 256 * 256;
+    p.ws_bytes = p.nsplit > 1 ? p.ticket_bytes + (size_t)p.units * p.nsplit * 16 * (g.d + 2) * sizeof(float) : 0;
+    return p;
+}
+static int64_t plan_tokens(const kvev_shape *sh, const PageGeom &g)
+{
+    const int64_t cap = (int64_t)g.max_pages << g.page_shift;
+    return sh->T > 0 ? std::min<int64_t>(sh->T, cap) : cap;
+}
+
+static int check_tables(const PageGeom &, const void *table, const void *length, const void *refs)
+{
+    return aligned4(table) && aligned4(length) && aligned4(refs) ? KVEV_OK : KVEV_ERR_INVALID_ARG;
+}
+
+static int rows_common(const kvev_shape *sh, const kvev_pages *pg, const void *K, const void *V, int Tn, const int32_t *start, const int32_t *n_new,
+                       const int32_t *table, void *pool, PageRowsArgs *a)
+{
+    memset(a, 0, sizeof *a);
+    const int rc = check_pages(sh, pg, &a->g);
+    if (rc) return rc;
+    if (!whole16(K) || !whole16(V) || !whole16(pool) || !aligned4(table) || !aligned4(start) || !aligned4_or_null(n_new) || Tn < 0)
+        return KVEV_ERR_INVALID_ARG;
+    if ((int64_t)sh->L * sh->B * a->g.Hkv * Tn > INT32_MAX) return KVEV_ERR_INVALID_ARG;
+    a->pool = static_cast<unsigned char *>(pool); a->table = table; a->start = start; a->n_new = n_new; a->Tn = Tn;
+    return KVEV_OK;
+}
+
+}  // namespace kvev
+
+using namespace kvev;
+
+extern "C" {
+
+size_t kvev_page_pool_bytes(const kvev_shape *sh, const kvev_pages *pg)
+{
+    PageGeom g;
+    return check_pages(sh, pg, &g) == KVEV_OK ? pool_bytes(g) : 0;
+}
+
+size_t kvev_page_workspace_bytes(int op, const kvev_shape *sh, const kvev_pages *pg, int n)
+{
+    PageGeom g;
+    if (check_pages(sh, pg, &g) != KVEV_OK || n < 0) return 0;
+    switch (op) {
+    case KVEV_OP_PAGE_ATTENTION:
+        return n == 0 ? 0 : plan_page_attn(sh, g, n, (int64_t)g.max_pages << g.page_shift).ws_bytes;
+    case KVEV_OP_PAGES_RESERVE:
+        return reserve_words(g) * 4;
+    case KVEV_OP_PAGES_COMPACT:
+        return compact_words(g) * 4;
+    default:
+        return 0;
+    }
+}
+
+int kvev_rotary(const kvev_shape *sh, const kvev_rotary_axes *axes, const float *freq, const int32_t *pos, int Tq, const void *Q,
+                const void *K, void *Q_out, void *K_out, int inverse, void *stream)
+{
+    const int rc = check_shape(sh, false);
+    if (rc) return rc;
+    if (!axes || axes->n_axes < 1 || axes->n_axes > 4 || Tq < 0 || (inverse != 0 && inverse != 1)) return KVEV_ERR_INVALID_ARG;
+    RotaryArgs a;
+    memset(&a, 0, sizeof a);
+    int64_t pairs = 0;
+    for (int x = 0; x < axes->n_axes; ++x) {
+        if (axes->section[x] < 0) return KVEV_ERR_INVALID_ARG;
+        pairs += axes->section[x];
+        a.end[x] = (int)std::min<int64_t>(pairs, sh->d);
+    }
+    for (int x = axes->n_axes; x < 4; ++x) a.end[x] = a.end[axes->n_axes - 1];
+    if (pairs < 1 || 2 * pairs > sh->d) return KVEV_ERR_INVALID_ARG;
+    if (axes->layout != KVEV_ROTARY_HALVES && axes->layout != KVEV_ROTARY_PAIRS) return KVEV_ERR_UNSUPPORTED;
+    if (!aligned4(freq) || !aligned4(pos) || (!Q && !K) || !Q != !Q_out || !K != !K_out) return KVEV_ERR_INVALID_ARG;
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(Q_out) || !aligned16(K_out)) return KVEV_ERR_INVALID_ARG;
+    if (Tq == 0) return KVEV_OK;
+    const int Hkv = kv_heads(sh);
+    if ((int64_t)sh->L * sh->B * sh->H * Tq > (int64_t)1 << 28 || (int64_t)axes->n_axes * sh->B * Tq > INT32_MAX) return KVEV_ERR_INVALID_ARG;
+    // in place, or apart from everything else
+    const size_t nq = Q ? (size_t)sh->L * sh->B * sh->H * Tq * sh->d * elem(sh) : 0, nk = K ? (size_t)sh->L * sh->B * Hkv * Tq * sh->d * elem(sh) : 0;
+    if (Q && Q != Q_out && overlap(Q, nq, Q_out, nq)) return KVEV_ERR_INVALID_ARG;
+    if (K && K != K_out && overlap(K, nk, K_out, nk)) return KVEV_ERR_INVALID_ARG;
+    if (Q && K && (overlap(Q_out, nq, K_out, nk) || overlap(Q, nq, K_out, nk) || overlap(Q_out, nq, K, nk))) return KVEV_ERR_INVALID_ARG;
+    a.Q = Q; a.K = K; a.Qo = Q_out; a.Ko = K_out; a.freq = freq; a.pos = pos;
+    a.L = sh->L; a.B = sh->B; a.H = sh->H; a.Hkv = Hkv; a.d = sh->d; a.Tq = Tq; a.n_axes = axes->n_axes;
+    a.pairs = (int)pairs; a.adjacent = axes->layout == KVEV_ROTARY_PAIRS; a.sign = inverse ? -1.f : 1.f;
+    const hipError_t e = launch_rotary(a, sh->dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? KVEV_OK : hip_fail(e);
+}
+
+int kvev_page_append(const kvev_shape *sh, const kvev_pages *pg, const void *K, const void *V, int Tn, const int32_t *start,
+                     const int32_t *n_new, const int32_t *table, void *pool, void *stream)
+{
+    PageRowsArgs a;
+    const int rc = rows_common(sh, pg, K, V, Tn, start, n_new, table, pool, &a);
+    if (rc || Tn == 0) return rc;
+    a.K = K; a.V = V;
+    const hipError_t e = launch_page_append(a, sh->dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? KVEV_OK : hip_fail(e);
+}
+
+int kvev_page_read(const kvev_shape *sh, const kvev_pages *pg, const void *pool, const int32_t *table, const int32_t *first,
+                   const int32_t *n, int Tn, void *K, void *V, void *stream)
+{
+    PageRowsArgs a;
+    const int rc = rows_common(sh, pg, K, V, Tn, first, n, table, const_cast<void *>(pool), &a);
+    if (rc || Tn == 0) return rc;
+    const size_t bytes = (size_t)sh->L * sh->B * a.g.Hkv * Tn * sh->d * elem(sh);
+    if (overlap(K, bytes, V, bytes)) return KVEV_ERR_INVALID_ARG;
+    a.Ko = K; a.Vo = V;
+    const hipError_t e = launch_page_read(a, sh->dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? KVEV_OK : hip_fail(e);
+}
+
+int kvev_page_attention(const kvev_shape *sh, const kvev_pages *pg, const void *Q, int Tq, const void *pool, const int32_t *table,
+                        const int32_t *length, const int32_t *first, const int32_t *q_start, const void *Kc, const void *Vc,
+                        const int32_t *count, int k_cap, void *O, void *ws, size_t ws_bytes, void *stream)
+{
+    PageAttnArgs a;
+    memset(&a, 0, sizeof a);
+    const int rc = check_pages(sh, pg, &a.g);
+    if (rc) return rc;
+    if (!whole16(Q) || !whole16(O) || !whole16(pool) || !aligned4(table) || !aligned4(length) || !aligned4_or_null(first) ||
+        !aligned4_or_null(q_start) || Tq < 0 || k_cap < 0)
+        return KVEV_ERR_INVALID_ARG;
+    if (k_cap > 0 && (!whole16(Kc) || !whole16(Vc) || !aligned4(count))) return KVEV_ERR_INVALID_ARG;
+    if ((int64_t)sh->L * sh->B * a.g.Hkv * k_cap > INT32_MAX) return KVEV_ERR_INVALID_ARG;
+    if (Tq == 0) return KVEV_OK;
+    if ((int64_t)sh->L * sh->B * sh->H * Tq > (int64_t)1 << 26) return KVEV_ERR_INVALID_ARG;
+    const size_t q_bytes = (size_t)sh->L * sh->B * sh->H * Tq * sh->d * elem(sh);
+    if (overlap(Q, q_bytes, O, q_bytes)) return KVEV_ERR_INVALID_ARG;
+    const PageAttnPlan p = plan_page_attn(sh, a.g, Tq, plan_tokens(sh, a.g));
+    if (p.ws_bytes > 0 && (!whole16(ws) || ws_bytes < p.ws_bytes)) return KVEV_ERR_WORKSPACE;
+    a.Q = Q; a.O = O; a.pool = static_cast<const unsigned char *>(pool); a.table = table; a.length = length; a.first = first; a.q_start = q_start;
+    if (k_cap > 0) { a.Kc = Kc; a.Vc = Vc; a.count = count; a.k_cap = k_cap; }
+    a.G = sh->H / a.g.Hkv; a.Tq = Tq; a.nsplit = p.nsplit; a.qtiles = p.qtiles; a.min_chunks = kPageMinChunks;
+    if (p.nsplit > 1) {
+        a.tickets = static_cast<int32_t *>(ws);
+        a.part = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + p.ticket_bytes);
+    }
+    a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)sh->d));
+    const hipError_t e = launch_page_attention(a, sh->dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? KVEV_OK : hip_fail(e);
+}
+
+int kvev_pages_reserve(const kvev_shape *sh, const kvev_pages *pg, const int32_t *n_new, int32_t *table, int32_t *length, int32_t *refs,
+                       void *pool, int32_t *start, int32_t *status, void *ws, size_t ws_bytes, void *stream)
+{
+    PagesArgs a;
+    memset(&a, 0, sizeof a);
+    int rc = check_pages(sh, pg, &a.g);
+    if (rc) return rc;
+    rc = check_tables(a.g, table, length, refs);
+    if (rc) return rc;
+    if (!aligned4(n_new) || !aligned4(start) || !aligned4(status) || !whole16(pool) || n_new == length || start == length || start == n_new)
+        return KVEV_ERR_INVALID_ARG;
+    if (!whole16(ws) || ws_bytes < reserve_words(a.g) * 4) return KVEV_ERR_WORKSPACE;
+    a.n_new = n_new; a.table = table; a.length = length; a.refs = refs; a.pool = static_cast<unsigned char *>(pool);
+    a.start = start; a.status = status; a.ws = static_cast<int32_t *>(ws);
+    const hipError_t e = launch_pages_reserve(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? KVEV_OK : hip_fail(e);
+}
+
+int kvev_pages_fork(const kvev_shape *sh, const kvev_pages *pg, const int32_t *src, const int32_t *dst, int n, int32_t *table,
+                    int32_t *length, int32_t *refs, int32_t *status, void *stream)
+{
+    PagesArgs a;
+    memset(&a, 0, sizeof a);
+    int rc = check_pages(sh, pg, &a.g);
+    if (rc) return rc;
+    rc = check_tables(a.g, table, length, refs);
+    if (rc) return rc;
+    if (n < 0 || n > sh->B || !aligned4(status) || !aligned4(src) || !aligned4(dst)) return KVEV_ERR_INVALID_ARG;
+    if (n == 0) return KVEV_OK;
+    a.src = src; a.dst = dst; a.n = n; a.table = table; a.length = length; a.refs = refs; a.status = status;
+    const hipError_t e = launch_pages_fork(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? KVEV_OK : hip_fail(e);
+}
+
+int kvev_pages_trim(const kvev_shape *sh, const kvev_pages *pg, const int32_t *rows, int n, const int32_t *first, const int32_t *keep,
+                    int32_t *table, int32_t *length, int32_t *refs, void *stream)
+{
+    PagesArgs a;
+    memset(&a, 0, sizeof a);
+    int rc = check_pages(sh, pg, &a.g);
+    if (rc) return rc;
+    rc = check_tables(a.g, table, length, refs);
+    if (rc) return rc;
+    if (n < 0 || n > sh->B || !aligned4_or_null(rows) || !aligned4_or_null(first) || !aligned4_or_null(keep)) return KVEV_ERR_INVALID_ARG;
+    if (n == 0) return KVEV_OK;
+    a.src = rows; a.n = n; a.first = first; a.keep = keep; a.table = table; a.length = length; a.refs = refs;
+    const hipError_t e = launch_pages_trim(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? KVEV_OK : hip_fail(e);
+}
+
+int kvev_pages_copy(const kvev_shape *sh, const kvev_pages *pg, void *pool, const int32_t *src, const int32_t *dst, int n,
+                    int32_t *status, void *stream)
+{
+    PagesArgs a;
+    memset(&a, 0, sizeof a);
+    const int rc = check_pages(sh, pg, &a.g);
+    if (rc) return rc;
+    if (n < 0 || n > pg->n_pages || !whole16(pool) || !aligned4(src) || !aligned4(dst) || !aligned4(status)) return KVEV_ERR_INVALID_ARG;
+    if (n == 0) return KVEV_OK;
+    a.pool = static_cast<unsigned char *>(pool); a.src = src; a.dst = dst; a.n = n; a.status = status;
+    const hipError_t e = launch_pages_copy(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? KVEV_OK : hip_fail(e);
+}
+
+int kvev_pages_compact(const kvev_shape *sh, const kvev_pages *pg, const void *pool, const int32_t *table, const int32_t *refs,
+                       const kvev_pages *to, void *to_pool, int32_t *to_table, int32_t *to_refs, int32_t *status, void *ws,
+                       size_t ws_bytes, void *stream)
+{
+    PagesArgs a;
+    PageGeom t;
+    memset(&a, 0, sizeof a);
+    int rc = check_pages(sh, pg, &a.g);
+    if (!rc) rc = check_pages(sh, to, &t);
+    if (rc) return rc;
+    if (t.page_shift != a.g.page_shift || t.max_pages != a.g.max_pages) return KVEV_ERR_INVALID_ARG;
+    if (!whole16(pool) || !whole16(to_pool) || !aligned4(table) || !aligned4(refs) || !aligned4(to_table) || !aligned4(to_refs) || !aligned4(status))
+        return KVEV_ERR_INVALID_ARG;
+    const size_t cells = (size_t)a.g.B * a.g.max_pages * 4;
+    if (overlap(pool, pool_bytes(a.g), to_pool, pool_bytes(t)) || overlap(refs, (size_t)a.g.n_pages * 4, to_refs, (size_t)t.n_pages * 4) ||
+        (table != to_table && overlap(table, cells, to_table, cells)))
+        return KVEV_ERR_INVALID_ARG;
+    if (!whole16(ws) || ws_bytes < compact_words(a.g) * 4) return KVEV_ERR_WORKSPACE;
+    a.pool = static_cast<unsigned char *>(const_cast<void *>(pool)); a.table = const_cast<int32_t *>(table); a.refs = const_cast<int32_t *>(refs);
+    a.to_pool = static_cast<unsigned char *>(to_pool); a.to_table = to_table; a.to_refs = to_refs; a.to_pages = t.n_pages;
+    a.status = status; a.ws = static_cast<int32_t *>(ws);
+    const hipError_t e = launch_pages_compact(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? KVEV_OK : hip_fail(e);
+}
+
+}  // extern "C"

@@ -20,11 +20,14 @@ namespace {
 
 // bound once by binding.py: types, what the current stream is asked of, and the library's entry points
 PyObject *g_shape_type, *g_rows_type, *g_tensor_type, *g_initialized, *g_get_device, *g_raw_stream;
-PyObject *s_is_contiguous, *s_data_ptr, *s_numel, *s_ptr;
+PyObject *g_pages_type, *g_axes_type, *g_f32, *g_bf16, *g_i32, *g_u8;       // (bind_pages)
+PyObject *s_is_contiguous, *s_data_ptr, *s_numel, *s_ptr, *s_dtype, *s_get_device;
 
-enum Entry { kPool, kGate, kGatePrepared, kSelect, kGated, kDense, kRetain, kCompact, kEntries };
+enum Entry { kPool, kGate, kGatePrepared, kSelect, kGated, kDense, kRetain, kCompact, kPoolBytes, kAppend, kRead, kPageAttn, kReserve, kFork, kTrim, kRotary, kEntries };
 const char *const kNames[kEntries] = {"kvev_chunk_pool", "kvev_lstm_gate", "kvev_lstm_gate_prepared", "kvev_select",
-                                      "kvev_gated_attention", "kvev_dense_attention", "kvev_retain", "kvev_compact_attention"};
+                                      "kvev_gated_attention", "kvev_dense_attention", "kvev_retain", "kvev_compact_attention",
+                                      "kvev_page_pool_bytes", "kvev_page_append", "kvev_page_read", "kvev_page_attention",
+                                      "kvev_pages_reserve", "kvev_pages_fork", "kvev_pages_trim", "kvev_rotary"};
 void *g_entry[kEntries];
 
 // Arguments are read one after the other; the first that is not plain leaves `plain` false, an exception leaves `error` true,
@@ -33,14 +36,16 @@ struct Reader {
     PyObject *const *args;
     Py_ssize_t n, at = 0;
     bool plain = true, error = false;
-    Py_buffer shape_view{};
-    bool has_view = false;
+    Py_buffer shape_view{}, more_view{};
+    bool has_view = false, has_more = false;
+    long device = -1;                      // current device, once stream() was asked
 
     Reader(PyObject *const *a, Py_ssize_t count, Py_ssize_t want) : args(a), n(count) { plain = g_shape_type && count == want; }
     Reader(const Reader &) = delete;
     ~Reader()
     {
         if (has_view) PyBuffer_Release(&shape_view);
+        if (has_more) PyBuffer_Release(&more_view);
     }
     bool ok() const { return plain && !error; }
     PyObject *next() { return args[at++]; }
@@ -54,6 +59,40 @@ struct Reader {
         has_view = true;
         if ((size_t)shape_view.len < sizeof(kvev_shape)) { plain = false; return nullptr; }
         return static_cast<const kvev_shape *>(shape_view.buf);
+    }
+    // the struct that goes with the shape (kvev_pages, kvev_rotary_axes)
+    template <class S> const S *more(PyObject *type)
+    {
+        if (!ok()) return nullptr;
+        PyObject *o = next();
+        if (!type || (PyObject *)Py_TYPE(o) != type) { plain = false; return nullptr; }
+        if (PyObject_GetBuffer(o, &more_view, PyBUF_SIMPLE) != 0) { error = true; return nullptr; }
+        has_more = true;
+        if ((size_t)more_view.len < sizeof(S)) { plain = false; return nullptr; }
+        return static_cast<const S *>(more_view.buf);
+    }
+    // a contiguous tensor of at least `least` elements of `dtype` on the current device (after stream()); what is not is left to
+    // binding.py, which says so
+    void *array(PyObject *dtype, size_t least, bool optional = false)
+    {
+        if (!ok()) return nullptr;
+        PyObject *o = next();
+        if (o == Py_None && optional) return nullptr;
+        if (!dtype || !PyObject_TypeCheck(o, (PyTypeObject *)g_tensor_type)) { plain = false; return nullptr; }
+        PyObject *t = PyObject_GetAttr(o, s_dtype);
+        if (!t) { error = true; return nullptr; }
+        const bool same = t == dtype;
+        Py_DECREF(t);
+        if (!same) { plain = false; return nullptr; }
+        if (ask(o, s_numel) < least && ok()) plain = false;
+        if (!ok()) return nullptr;
+        PyObject *d = PyObject_VectorcallMethod(s_get_device, &o, 1 | PY_VECTORCALL_ARGUMENTS_OFFSET, nullptr);
+        if (!d) { error = true; return nullptr; }
+        const long at = PyLong_Check(d) ? PyLong_AsLong(d) : -1;
+        Py_DECREF(d);
+        if (at == -1 && PyErr_Occurred()) PyErr_Clear();
+        if (at < 0 || at != device) { plain = false; return nullptr; }
+        return address(o, true);
     }
     int integer()
     {
@@ -151,6 +190,8 @@ struct Reader {
         if (!is_up) { plain = false; return nullptr; }
         PyObject *dev = PyObject_CallNoArgs(g_get_device);
         if (!dev) { error = true; return nullptr; }
+        device = PyLong_Check(dev) ? PyLong_AsLong(dev) : -1;
+        if (device == -1 && PyErr_Occurred()) PyErr_Clear();
         PyObject *r = PyObject_CallOneArg(g_raw_stream, dev);
         Py_DECREF(dev);
         if (!r) { error = true; return nullptr; }
@@ -293,6 +334,177 @@ PyObject *compact_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
     return r.run([&] { return ENTRY(kCompact, kvev_compact_attention)(sh, Q, Tq, Kw, Vw, first, Kc, Vc, (int32_t *)count, k_cap, causal, O, ws, bytes, st); });
 }
 
+// ---- the paged cache: its calls check sizes, element types and device as well ----
+struct PageReader : Reader {
+    void *st;
+    const kvev_shape *sh;
+    const kvev_pages *pg = nullptr;
+
+    PageReader(PyObject *const *a, Py_ssize_t n, Py_ssize_t want) : Reader(a, n, want)
+    {
+        st = stream();
+        sh = shape();
+    }
+    const kvev_pages *pages() { return pg = more<kvev_pages>(g_pages_type); }
+    int heads() { return sh->H_kv > 0 ? sh->H_kv : sh->H; }
+    // a product of counts; what no tensor has if one is negative (the library then says what is wrong) or it is too large
+    static size_t product(const long long (&v)[5])
+    {
+        unsigned __int128 p = 1;
+        for (long long x : v) {
+            if (x < 0) return SIZE_MAX;
+            p *= (unsigned long long)x;
+            if (p > SIZE_MAX / 4) return SIZE_MAX;
+        }
+        return (size_t)p;
+    }
+    void *ints(long long n, bool optional = false) { return array(g_i32, n < 0 ? SIZE_MAX : (size_t)n, optional); }
+    void *rows(int h, int n, bool optional = false)
+    {
+        if (!ok()) return nullptr;
+        return array(sh->dtype == KVEV_F32 ? g_f32 : sh->dtype == KVEV_BF16 ? g_bf16 : nullptr, product({sh->L, sh->B, h, n, sh->d}), optional);
+    }
+    void *table() { return ok() ? ints((long long)sh->B * pg->max_pages) : nullptr; }
+    void *batch(bool optional = false) { return ok() ? ints(sh->B, optional) : nullptr; }
+    void *refs() { return ok() ? ints(pg->n_pages) : nullptr; }
+    void *pool() { return ok() ? array(g_u8, ENTRY(kPoolBytes, kvev_page_pool_bytes)(sh, pg)) : nullptr; }
+    void *bytes(size_t &n)
+    {
+        n = 0;
+        if (!ok()) return nullptr;
+        PyObject *o = args[at];
+        void *p = array(g_u8, 0, true);
+        if (ok() && p) n = ask(o, s_numel);
+        return p;
+    }
+};
+
+PyObject *page_append(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    PageReader r(args, n, 9);
+    if (!r.pages()) return r.run([] { return 0; });
+    const Py_ssize_t tensors = r.at;         // (their size is known once Tn is)
+    r.at += 2;
+    const int Tn = r.integer();
+    const Py_ssize_t rest = r.at;
+    r.at = tensors;
+    void *K = r.ok() ? r.rows(r.heads(), Tn) : nullptr, *V = r.ok() ? r.rows(r.heads(), Tn) : nullptr;
+    r.at = rest;
+    void *start = r.batch(), *n_new = r.batch(true), *table = r.table(), *pool = r.pool();
+    return r.run([&] { return ENTRY(kAppend, kvev_page_append)(r.sh, r.pg, K, V, Tn, (int32_t *)start, (int32_t *)n_new, (int32_t *)table, pool, r.st); });
+}
+
+PyObject *page_read(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    PageReader r(args, n, 9);
+    if (!r.pages()) return r.run([] { return 0; });
+    void *pool = r.pool(), *table = r.table(), *first = r.batch(), *count = r.batch(true);
+    const int Tn = r.integer();
+    void *K = r.ok() ? r.rows(r.heads(), Tn) : nullptr, *V = r.ok() ? r.rows(r.heads(), Tn) : nullptr;
+    return r.run([&] { return ENTRY(kRead, kvev_page_read)(r.sh, r.pg, pool, (int32_t *)table, (int32_t *)first, (int32_t *)count, Tn, K, V, r.st); });
+}
+
+PyObject *page_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    PageReader r(args, n, 15);
+    if (!r.pages()) return r.run([] { return 0; });
+    const Py_ssize_t q_at = r.at++;
+    const int Tq = r.integer();
+    const Py_ssize_t rest = r.at;
+    r.at = q_at;
+    void *Q = r.ok() ? r.rows(r.sh->H, Tq) : nullptr;
+    r.at = n - 1;
+    const int k_cap = r.integer();
+    r.at = rest;
+    void *pool = r.pool(), *table = r.table(), *length = r.batch(), *O = r.ok() ? r.rows(r.sh->H, Tq) : nullptr;
+    size_t bytes;
+    void *ws = r.bytes(bytes), *first = r.batch(true), *q_start = r.batch(true);
+    const bool none = k_cap == 0;
+    void *Kc = r.ok() ? r.rows(r.heads(), k_cap, none) : nullptr, *Vc = r.ok() ? r.rows(r.heads(), k_cap, none) : nullptr;
+    void *count = r.ok() ? r.ints((long long)r.sh->L * r.sh->B * r.heads(), none) : nullptr;
+    return r.run([&] {
+        return ENTRY(kPageAttn, kvev_page_attention)(r.sh, r.pg, Q, Tq, pool, (int32_t *)table, (int32_t *)length, (int32_t *)first, (int32_t *)q_start, Kc, Vc,
+                                                     (int32_t *)count, k_cap, O, ws, bytes, r.st);
+    });
+}
+
+PyObject *pages_reserve(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    PageReader r(args, n, 10);
+    if (!r.pages()) return r.run([] { return 0; });
+    void *n_new = r.batch(), *table = r.table(), *length = r.batch(), *refs = r.refs(), *pool = r.pool(), *start = r.batch(), *status = r.ints(1);
+    size_t bytes;
+    void *ws = r.bytes(bytes);
+    return r.run([&] {
+        return ENTRY(kReserve, kvev_pages_reserve)(r.sh, r.pg, (int32_t *)n_new, (int32_t *)table, (int32_t *)length, (int32_t *)refs, pool, (int32_t *)start,
+                                                   (int32_t *)status, ws, bytes, r.st);
+    });
+}
+
+PyObject *pages_fork(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    PageReader r(args, n, 9);
+    if (!r.pages()) return r.run([] { return 0; });
+    const Py_ssize_t lists = r.at;
+    r.at += 2;
+    const int count = r.integer();
+    const Py_ssize_t rest = r.at;
+    r.at = lists;
+    void *src = r.ints(count), *dst = r.ints(count);
+    r.at = rest;
+    void *table = r.table(), *length = r.batch(), *refs = r.refs(), *status = r.ints(1);
+    return r.run([&] {
+        return ENTRY(kFork, kvev_pages_fork)(r.sh, r.pg, (int32_t *)src, (int32_t *)dst, count, (int32_t *)table, (int32_t *)length, (int32_t *)refs, (int32_t *)status, r.st);
+    });
+}
+
+PyObject *pages_trim(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    PageReader r(args, n, 9);
+    if (!r.pages()) return r.run([] { return 0; });
+    const Py_ssize_t list = r.at++;
+    const int count = r.integer();
+    const Py_ssize_t rest = r.at;
+    r.at = list;
+    void *rows = r.ints(count, true);
+    r.at = rest;
+    void *first = r.ints(count, true), *keep = r.ints(count, true), *table = r.table(), *length = r.batch(), *refs = r.refs();
+    return r.run([&] {
+        return ENTRY(kTrim, kvev_pages_trim)(r.sh, r.pg, (int32_t *)rows, count, (int32_t *)first, (int32_t *)keep, (int32_t *)table, (int32_t *)length, (int32_t *)refs, r.st);
+    });
+}
+
+PyObject *rotary(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    PageReader r(args, n, 10);
+    const kvev_rotary_axes *ax = r.more<kvev_rotary_axes>(g_axes_type);
+    if (!ax) return r.run([] { return 0; });
+    long long pairs = 0;
+    for (int i = 0; i < ax->n_axes && i < 4; ++i) pairs += ax->section[i];
+    const Py_ssize_t front = r.at;
+    r.at += 2;
+    const int Tq = r.integer();
+    const Py_ssize_t rest = r.at;
+    r.at = front;
+    void *freq = r.array(g_f32, pairs < 0 ? SIZE_MAX : (size_t)pairs);
+    void *pos = r.ok() ? r.array(g_i32, PageReader::product({ax->n_axes, r.sh->B, Tq, 1, 1})) : nullptr;
+    r.at = rest;
+    void *Q = r.ok() ? r.rows(r.sh->H, Tq, true) : nullptr, *K = r.ok() ? r.rows(r.heads(), Tq, true) : nullptr;
+    void *Qo = r.ok() ? r.rows(r.sh->H, Tq, true) : nullptr, *Ko = r.ok() ? r.rows(r.heads(), Tq, true) : nullptr;
+    const int inverse = r.integer();
+    return r.run([&] { return ENTRY(kRotary, kvev_rotary)(r.sh, ax, (float *)freq, (int32_t *)pos, Tq, Q, K, Qo, Ko, inverse, r.st); });
+}
+
+// bind_pages(Pages, RotaryAxes, float32, bfloat16, int32, uint8), before bind
+PyObject *bind_pages(PyObject *, PyObject *args)
+{
+    PyObject *pages, *axes, *f32, *bf16, *i32, *u8;
+    if (!PyArg_ParseTuple(args, "O!O!OOOO", &PyType_Type, &pages, &PyType_Type, &axes, &f32, &bf16, &i32, &u8)) return nullptr;
+    Py_INCREF(pages); Py_INCREF(axes); Py_INCREF(f32); Py_INCREF(bf16); Py_INCREF(i32); Py_INCREF(u8);
+    g_pages_type = pages; g_axes_type = axes; g_f32 = f32; g_bf16 = bf16; g_i32 = i32; g_u8 = u8;
+    Py_RETURN_NONE;
+}
+
 // bind(Shape, RowsFrom, Tensor, is_initialized, get_device, raw_stream, {name: address})
 PyObject *bind(PyObject *, PyObject *args)
 {
@@ -317,7 +529,9 @@ PyObject *bind(PyObject *, PyObject *args)
 PyMethodDef g_methods[] = {
     FAST("chunk_pool", chunk_pool), FAST("lstm_gate", lstm_gate), FAST("lstm_gate_prepared", lstm_gate_prepared), FAST("select", select_),
     FAST("gated_attention", gated_attention), FAST("dense_attention", dense_attention), FAST("retain", retain),
-    FAST("compact_attention", compact_attention), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+    FAST("compact_attention", compact_attention), FAST("page_append", page_append), FAST("page_read", page_read),
+    FAST("page_attention", page_attention), FAST("pages_reserve", pages_reserve), FAST("pages_fork", pages_fork), FAST("pages_trim", pages_trim),
+    FAST("rotary", rotary), {"bind_pages", bind_pages, METH_VARARGS, nullptr}, {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", "Marshalling of calls into libkvev.so.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -328,6 +542,8 @@ PyMODINIT_FUNC PyInit__native(void)
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_numel = PyUnicode_InternFromString("numel");
     s_ptr = PyUnicode_InternFromString("ptr");
-    if (!s_is_contiguous || !s_data_ptr || !s_numel || !s_ptr) return nullptr;
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_get_device = PyUnicode_InternFromString("get_device");
+    if (!s_is_contiguous || !s_data_ptr || !s_numel || !s_ptr || !s_dtype || !s_get_device) return nullptr;
     return PyModule_Create(&g_module);
 }

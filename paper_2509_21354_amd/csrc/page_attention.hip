@@ -1,0 +1,398 @@
+// Attention over a paged 4-bit cache: Eq. 1 of the paper for every batch row over the kept summaries of a compact store (in the
+// storage type) and the tokens [first, length) of its pages.
+//
+// With keys and values in 4 bits a row of d = 128 is 68 bytes, and a compute unit has to take one of them every 5 clocks to keep
+// up with the memory: too many elements for the vector unit even for a single query.  Both products therefore run on the matrix
+// cores (v_mfma_f32_16x16x32_bf16) at any number of queries, transposed as in the frame kernels so that the softmax weights stay
+// in their lanes:
+//   S^T = K Q^T   A = 16 tokens, B = 16 queries.  Lane (row l % 16, block l / 16) loads a contiguous quarter of its token's
+//                 codes, which lies in one block of 32 and so has one scale, and the hardware conversion gives bf16 with the
+//                 scale in it, exactly.  (The contraction index may be permuted freely: step kk of the product takes elements
+//                 8 kk .. 8 kk + 7 of every lane's quarter, and the queries are loaded the same way.)
+//   O^T = V^T P^T A = V^T through LDS: values converted as above go to a wave's own 32 rows and come back by the transposing
+//                 load; B = the weights where the first product left them.
+// A wave takes chunks of 64 rows; the four waves of a workgroup take chunks in turn and meet in LDS at the end, the workgroups
+// that share a unit's rows meet in scratch (partials, a ticket, the last one to arrive merges in split order).
+// fp32: the queries enter as three bf16 terms of 8 bits, the weights likewise, rows of the store too (products of terms below
+// 2^-24 left out).  bf16: the weights enter as two terms.
+//
+// Values that are not finite: a block of the cache that held one has the scale byte 255 and reads as NaN.  Such keys make their
+// token's scores NaN, which a query that must not see the token replaces.  Values would reach every query of the tile as 0 * NaN,
+// so blocks of values marked 255 enter the product as zeros, and the outputs of the queries that do see the token are set to NaN
+// at the end.
+#include "kernels.hpp"
+#include "pages.hpp"
+#include <utility>
+
+namespace kvev {
+
+#ifdef __HIP_DEVICE_COMPILE__
+__device__ __forceinline__ void store_device(float *p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float load_device(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// fp32 values cut into three bf16 terms of 8 significant bits each (their sum is the value)
+__device__ __forceinline__ void cut3(const float (&x)[8], bf16x8_t (&t)[3])
+{
+    uint32_t w[3][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t c[3][2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float v = x[2 * i + e];
+            const uint32_t h = __float_as_uint(v) & 0xFFFF0000u;
+            const bool finite = (h & kInfBits) != kInfBits;
+            const float r = finite ? v - __uint_as_float(h) : 0.f;
+            const uint32_t m = __float_as_uint(r) & 0xFFFF0000u;
+            // (a NaN whose payload sits in the low half stays one)
+            c[0][e] = (finite ? h : __float_as_uint(v + v) ) >> 16;
+            c[1][e] = m >> 16;
+            c[2][e] = __float_as_uint(r - __uint_as_float(m)) >> 16;
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) w[k][i] = c[k][0] | c[k][1] << 16;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) t[k] = __builtin_bit_cast(bf16x8_t, make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]));
+}
+
+// weights (0 .. 1) as N bf16 terms: rounded, then what the rounding left
+template <int N> __device__ __forceinline__ void cut_weights(const float (&p)[8], bf16x8_t (&t)[N])
+{
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = p[e];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = pack_bf16x2(r[2 * i], r[2 * i + 1]);
+            r[2 * i] -= __uint_as_float(w[i] << 16);
+            r[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+        t[k] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
+    }
+}
+
+template <typename T> struct Terms;
+template <> struct Terms<bf16_t> {
+    static constexpr int Q = 1, P = 2;
+    static __device__ __forceinline__ void load(const bf16_t *p, bf16x8_t (&t)[1]) { t[0] = *reinterpret_cast<const bf16x8_t *>(p); }
+};
+template <> struct Terms<float> {
+    static constexpr int Q = 3, P = 3;
+    static __device__ __forceinline__ void load(const float *p, bf16x8_t (&t)[3])
+    {
+        float v[8];
+        VecLoad<float, 8>::run(p, v);
+        cut3(v, t);
+    }
+};
+
+// where in a group's keys or values lane (token n, quarter gr) finds its codes
+template <int D> __device__ __forceinline__ int lane_offset(int n, int gr) { return n * (D / 2) + gr * (D / 8); }
+template <int D> struct Codes;            // a lane's quarter of a token's codes
+template <> struct Codes<128> { typedef u32x4_t type; };
+template <> struct Codes<64> { typedef u32x2_t type; };
+#endif
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void page_attention_kernel(PageAttnArgs a)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr int NQ = Terms<T>::Q, NP = Terms<T>::P, KS = D / 32, DT = D / 16, NB = D / 32;
+    constexpr int RPV = D + 16;                  // pitch of the staged values (see the frame kernels)
+    constexpr int OP = D + 4;                    // pitch of the waves' outputs
+    constexpr int STAGE = 32 * RPV * 2, OUT = 16 * OP * 4;
+    __shared__ __align__(16) unsigned char s_mem[4 * (STAGE > OUT ? STAGE : OUT)];
+    __shared__ float s_m[4][16], s_l[4][16];
+
+    const PageGeom &g = a.g;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, gr = lane >> 4;
+    uint32_t blk = blockIdx.x;
+    const int split = (int)(blk % (uint32_t)a.nsplit); blk /= (uint32_t)a.nsplit;
+    const int unit = (int)blk;
+    const int qt = unit % a.qtiles, s = unit / a.qtiles, h = s % g.Hkv, lb = s / g.Hkv, b = lb % g.B, l = lb / g.B;
+    const int R = a.G * a.Tq, cap = g.max_pages << g.page_shift;
+
+    // the rows of this unit in chunks of 64: the store's, then the pages' from the chunk of `first` on
+    const int len = min(max(a.length[b], 0), cap), first = a.first ? min(max(a.first[b], 0), len) : 0;
+    const int kept = a.count ? min(max(a.count[s], 0), a.k_cap) : 0;
+    const int sc = (kept + 63) >> 6, base0 = first & ~63, pc = (len - base0 + 63) >> 6, chunks = sc + pc;
+    const int per = max(a.min_chunks, (chunks + a.nsplit - 1) / a.nsplit), active = max(1, (chunks + per - 1) / per);
+    if (split >= active) return;
+    const int c0 = split * per, c1 = min(chunks, c0 + per);
+
+    // this lane's query, and the last token that it sees
+    const int r = qt * 16 + n, rc = min(r, R - 1), gq = rc / a.Tq, tq = rc - gq * a.Tq;
+    const size_t orow = (((size_t)lb * g.Hkv + h) * a.G + gq) * a.Tq + tq;
+    int lim = len - 1;
+    if (a.q_start) lim = (int)min<int64_t>(lim, (int64_t)a.q_start[b] + tq);
+    bf16x8_t qf[KS][NQ];
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) Terms<T>::load(static_cast<const T *>(a.Q) + orow * D + gr * (D / 4) + kk * 8, qf[kk]);
+
+    float m = -INFINITY, lsum = 0.f;             // scaled running maximum and this lane's part of the sum, of query n
+    f32x4_t o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    uint32_t nan_blocks = 0;                     // blocks of d whose values are NaN in a token that query n sees
+
+    bf16_t *s_v = reinterpret_cast<bf16_t *>(s_mem + wave * STAGE);
+    const float c = a.scale_log2e;
+    const size_t block = block_bytes(g);
+    const unsigned char *pool = a.pool + ((size_t)l * g.n_pages * g.Hkv + h) * block;
+    const int32_t *table = a.table + (size_t)b * g.max_pages;
+
+    // the weights of a chunk from its scores (hidden ones: -inf), and the running state
+    auto soft = [&](f32x4_t (&st)[4], bf16x8_t (&pb)[2][NP]) __attribute__((always_inline)) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, st[kt][e]);
+        mx = rows_max(mx) * c;
+        const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
+        if (__any(m_new > m)) {
+            const float alpha = __builtin_amdgcn_exp2f(m - ref);
+            lsum *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[dt][e] *= alpha;
+            m = m_new;
+        }
+        // (The multiply-add leaves the rounding of the maximum's product in every weight, a factor that the normaliser shares.
+        // Where it is no longer near 1, the products are rounded first.)
+        float cc = c;
+        if (__any(fabsf(ref) > 0x1p20f)) {
+            cc = 1.0f;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) st[kt][e] *= c;
+        }
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+            float p[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(fmaf(st[2 * h2 + (e >> 2)][e & 3], cc, -ref));
+                lsum += p[e];
+            }
+            cut_weights<NP>(p, pb[h2]);
+        }
+    };
+    // O^T += V^T P^T over the 32 staged rows, for one term of the values (VT: which) with the weights' terms that matter
+    auto values = [&](const bf16x8_t (&pb)[NP], int skip) __attribute__((always_inline)) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            const bf16_t *src = s_v + (4 * gr + (n >> 2)) * RPV + dt * 16 + 4 * (n & 3);
+            const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)src);
+            const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)(src + 16 * RPV));
+            const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int k = NP - 1; k >= 0; --k)
+                if (k + skip < NP) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[k], o[dt], 0, 0, 0);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+
+    for (int ch = c0 + wave; ch < c1; ch += 4) {
+        f32x4_t st[4];
+        bf16x8_t pb[2][NP];
+        if (ch < sc) {
+            // ---- 64 rows of the store ----
+            const T *Kc = static_cast<const T *>(a.Kc) + (size_t)s * a.k_cap * D, *Vc = static_cast<const T *>(a.Vc) + (size_t)s * a.k_cap * D;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                const int j0 = ch * 64 + kt * 16, j = min(j0 + n, kept - 1);
+                st[kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kk = 0; kk < KS; ++kk) {
+                    bf16x8_t kf[NQ];
+                    Terms<T>::load(Kc + (size_t)j * D + gr * (D / 4) + kk * 8, kf);
+#pragma unroll
+                    for (int x = NQ - 1; x >= 0; --x)
+#pragma unroll
+                        for (int y = NQ - 1 - x; y >= 0; --y) st[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x], qf[kk][y], st[kt], 0, 0, 0);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j0 + 4 * gr + e >= kept) st[kt][e] = -INFINITY;
+            }
+            soft(st, pb);
+#pragma unroll
+            for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+                for (int x = NQ - 1; x >= 0; --x) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int j = ch * 64 + h2 * 32 + i * 16 + n;
+#pragma unroll
+                        for (int kk = 0; kk < KS; ++kk) {
+                            bf16x8_t vf[NQ];
+                            Terms<T>::load(Vc + (size_t)min(j, kept - 1) * D + gr * (D / 4) + kk * 8, vf);
+                            if (j >= kept) vf[x] = __builtin_bit_cast(bf16x8_t, make_uint4(0u, 0u, 0u, 0u));
+                            *reinterpret_cast<bf16x8_t *>(s_v + (i * 16 + n) * RPV + gr * (D / 4) + kk * 8) = vf[x];
+                        }
+                    }
+                    values(pb[h2], x);
+                }
+            continue;
+        }
+        // ---- 64 tokens of the pages ----
+        typedef typename Codes<D>::type codes_t;
+        const int t0 = base0 + (ch - sc) * 64;
+        codes_t kc[4], vc[4];
+        uint32_t sk[4], sv[4];
+        bool there[4];                            // this lane's token of the group is one that some query may see
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = t0 + 16 * i, pi = t >> g.page_shift;
+            int page = pi < g.max_pages ? table[pi] : -1;
+            const bool ok = (uint32_t)page < (uint32_t)g.n_pages;
+            there[i] = ok && t + n >= first && t + n < len;
+            page = ok ? page : 0;
+            const unsigned char *p = pool + (size_t)page * g.Hkv * block + (size_t)((t & ((1 << g.page_shift) - 1)) >> 4) * group_bytes(D);
+            kc[i] = *reinterpret_cast<const codes_t *>(p + lane_offset<D>(n, gr));
+            vc[i] = *reinterpret_cast<const codes_t *>(p + 8 * D + lane_offset<D>(n, gr));
+            const uint32_t sc2 = *reinterpret_cast<const uint16_t *>(p + 16 * D + (n * NB + gr * NB / 4) * 2);
+            sk[i] = sc2 & 255u;
+            sv[i] = sc2 >> 8;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (!there[i]) { kc[i] = codes_t{}; vc[i] = codes_t{}; sk[i] = sv[i] = 127u; }
+        }
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+            st[kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kk = 0; kk < KS; ++kk) {
+                const bf16x8_t kf = unpack8(kc[kt][kk], scale_of(sk[kt]));
+#pragma unroll
+                for (int y = NQ - 1; y >= 0; --y) st[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[kk][y], st[kt], 0, 0, 0);
+            }
+            // tokens of this group that lie in a page, [first, len), as the lanes that loaded them saw it
+            const uint32_t held = (uint32_t)(__ballot(there[kt]) & 0xFFFFu);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (!(held >> (4 * gr + e) & 1) || t0 + 16 * kt + 4 * gr + e > lim) st[kt][e] = -INFINITY;
+        }
+        soft(st, pb);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint64_t bad = __ballot(sv[i] == kNanScale);
+            while (bad) {                        // (rare)
+                const int x = __builtin_ctzll(bad);
+                bad &= bad - 1;
+                if (t0 + 16 * i + (x & 15) <= lim) nan_blocks |= 1u << ((x >> 4) * NB / 4);
+            }
+            if (sv[i] == kNanScale) { vc[i] = codes_t{}; sv[i] = 127u; }
+        }
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int kk = 0; kk < KS; ++kk)
+                    *reinterpret_cast<bf16x8_t *>(s_v + (i * 16 + n) * RPV + gr * (D / 4) + kk * 8) = unpack8(vc[2 * h2 + i][kk], scale_of(sv[2 * h2 + i]));
+            values(pb[h2], 0);
+        }
+    }
+    if (nan_blocks) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+            if (nan_blocks >> (dt / 2) & 1) o[dt] = f32x4_t{NAN, NAN, NAN, NAN};
+    }
+
+    // ---- the waves meet ----
+    __syncthreads();                             // (the staging rows become the waves' outputs)
+    float *s_o = reinterpret_cast<float *>(s_mem);
+    lsum = rows_sum(lsum);
+    if (gr == 0) { s_m[wave][n] = m; s_l[wave][n] = lsum; }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t *>(s_o + (wave * 16 + n) * OP + dt * 16 + 4 * gr) = o[dt];
+    __syncthreads();
+    constexpr int EPT = D / 16;                  // elements of a thread: 16 threads per query
+    const int oq = tid >> 4, oe = (tid & 15) * EPT, orr = qt * 16 + oq;
+    float M = s_m[0][oq];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) M = fmaxf(M, s_m[w][oq]);
+    const float Mr = M == -INFINITY ? 0.f : M;
+    float L = 0.f, acc[EPT] = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(s_m[w][oq] - Mr);
+        L += s_l[w][oq] * f;
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) acc[e] += s_o[(w * 16 + oq) * OP + oe + e] * f;
+    }
+    const int ogq = orr / a.Tq, otq = orr - ogq * a.Tq;
+    T *O = static_cast<T *>(a.O) + ((((size_t)lb * g.Hkv + h) * a.G + ogq) * a.Tq + otq) * D + oe;
+    if (active == 1) {
+        if (orr < R) {
+            const float inv = L == 0.f ? 0.f : 1.0f / L;         // (no rows: 0; a NaN stays one)
+#pragma unroll
+            for (int e = 0; e < EPT; ++e) Storage<T>::store(O + e, L == 0.f ? 0.f : acc[e] * inv);
+        }
+        return;
+    }
+    float *part = a.part + (((size_t)unit * a.nsplit + split) * 16 + oq) * (D + 2);
+    if (orr < R) {
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) store_device(part + oe + e, acc[e]);
+        if (oe == 0) { store_device(part + D, M); store_device(part + D + 1, L); }
+    }
+    // ---- the workgroups meet: as in decode attention ----
+    __shared__ int s_last;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // this wave's stores have completed
+    __syncthreads();
+    if (tid == 0) s_last = __hip_atomic_fetch_add(a.tickets + unit, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == active - 1;
+    __syncthreads();
+    if (!s_last) return;
+    if (tid == 0) __hip_atomic_store(a.tickets + unit, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (orr >= R) return;
+    part = a.part + ((size_t)unit * a.nsplit * 16 + oq) * (D + 2);
+    M = -INFINITY;
+    for (int x = 0; x < active; ++x) M = fmaxf(M, load_device(part + (size_t)x * 16 * (D + 2) + D));
+    const float ref = M == -INFINITY ? 0.f : M;
+    L = 0.f;
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) acc[e] = 0.f;
+    for (int x = 0; x < active; ++x) {
+        const float *pp = part + (size_t)x * 16 * (D + 2);
+        const float f = __builtin_amdgcn_exp2f(load_device(pp + D) - ref);
+        L += load_device(pp + D + 1) * f;
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) acc[e] += load_device(pp + oe + e) * f;
+    }
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) Storage<T>::store(O + e, L == 0.f ? 0.f : acc[e] * inv);
+#endif
+}
+
+hipError_t launch_page_attention(const PageAttnArgs &a, int dtype, hipStream_t st)
+{
+    const int64_t blocks = (int64_t)a.g.L * a.g.B * a.g.Hkv * a.qtiles * a.nsplit;
+    const dim3 grid((unsigned)blocks), block(256);
+    if (dtype == KVEV_F32) {
+        if (a.g.d == 128) hipLaunchKernelGGL((page_attention_kernel<float, 128>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((page_attention_kernel<float, 64>), grid, block, 0, st, a);
+    } else {
+        if (a.g.d == 128) hipLaunchKernelGGL((page_attention_kernel<bf16_t, 128>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((page_attention_kernel<bf16_t, 64>), grid, block, 0, st, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace kvev

@@ -1,0 +1,347 @@
+// Handing out, sharing, freeing and packing the pages of a 4-bit cache.
+//
+// A page is in use while refs[page] > 0, the number of table entries that name it; there is no list of free pages to keep in
+// order.  Whoever needs pages takes the free ones of lowest index, in the order of the rows, so a call's outcome depends on
+// nothing but what the arrays held before it.  Atomics are integer additions and exchanges whose order does not show.
+// Tables and counts are small (a few bytes per page): those kernels are chains of memory round trips, one workgroup each where
+// they have to see all rows.  Copies move whole 16-byte pieces at the rate of the memory.
+#include "kernels.hpp"
+#include "pages.hpp"
+
+namespace kvev {
+
+constexpr int kStatusNoPages = 1, kStatusRow = 2, kStatusPair = 4;     // bits of the status word (kvev.h)
+// words of the reserve scratch, after a head of 64 (word 0: rows to copy)
+enum { kNeed = 0, kAt = 1, kFrom = 2, kTo = 3, kGroups = 4 };
+constexpr int kHead = 64;
+
+// exclusive sum over the threads of a workgroup of NT; `total` receives the sum of all
+template <int NT> __device__ __forceinline__ int block_scan(int v, int &total)
+{
+    __shared__ int s_w[NT / 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int x = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    __syncthreads();                       // (s_w of a scan before is read)
+    if (lane == 63) s_w[wave] = x;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        const int y = s_w[w];
+        before += w < wave ? y : 0;
+        total += y;
+    }
+    return before + x - v;
+}
+
+__device__ __forceinline__ int pages_of(int tokens, int shift) { return (tokens + (1 << shift) - 1) >> shift; }
+
+// Room for n_new[b] more tokens in every row.
+__global__ __launch_bounds__(1024) void reserve_kernel(PagesArgs a)
+{
+    const PageGeom &g = a.g;
+    const int tid = threadIdx.x, shift = g.page_shift, cap = g.max_pages << shift, in_page = (1 << shift) - 1;
+    int32_t *rows = a.ws + kHead, *list = rows + (size_t)5 * g.B;
+    __shared__ int s_status;
+    if (tid == 0) s_status = 0;
+    __syncthreads();
+
+    // what every row needs, and where its pages begin in the list of those found
+    int total = 0;
+    for (int b0 = 0; b0 < g.B; b0 += 1024) {
+        const int b = b0 + tid;
+        int need = 0;
+        if (b < g.B) {
+            const int len = a.length[b], n = max(a.n_new[b], 0);
+            int from = -1, bad = len < 0 || len > cap || n > cap - len;
+            if (!bad && n > 0) {
+                need = pages_of(len + n, shift) - pages_of(len, shift);
+                if (len & in_page) {       // goes on in a page: in a copy of it if others share it
+                    const int page = a.table[(size_t)b * g.max_pages + (len >> shift)];
+                    if ((uint32_t)page >= (uint32_t)g.n_pages) bad = 1;
+                    else if (a.refs[page] > 1) { from = page; ++need; }
+                }
+            }
+            if (bad) { need = 0; atomicOr(&s_status, kStatusRow); }
+            rows[kNeed * g.B + b] = bad ? -1 : need;
+            rows[kFrom * g.B + b] = from;
+        }
+        int sum;
+        const int at = block_scan<1024>(need, sum);
+        if (b < g.B) rows[kAt * g.B + b] = total + at;
+        total += sum;
+    }
+
+    // the free pages of lowest index
+    int found = 0;
+    constexpr int PER = 8;
+    for (int p0 = 0; found < total && p0 < g.n_pages; p0 += 1024 * PER) {
+        const int p = p0 + tid * PER;
+        int free_bits = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (p + i < g.n_pages && a.refs[p + i] == 0) free_bits |= 1 << i;
+        int sum, at = block_scan<1024>(__popc(free_bits), sum);
+        at += found;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (free_bits >> i & 1) {
+                if (at < total) list[at] = p + i;
+                ++at;
+            }
+        found += sum;
+    }
+    __syncthreads();
+    const bool enough = found >= total;
+
+    // tables, counts, lengths; the copies to make
+    __shared__ int s_moves;
+    if (tid == 0) s_moves = 0;
+    __syncthreads();
+    const int lane = tid & 63;
+    for (int b = tid >> 6; b < g.B; b += 16) {
+        const int need = rows[kNeed * g.B + b], len = a.length[b];
+        if (need < 0 || !enough) {
+            if (lane == 0) a.start[b] = -1;
+            continue;
+        }
+        const int n = max(a.n_new[b], 0), at = rows[kAt * g.B + b], from = rows[kFrom * g.B + b];
+        int32_t *row = a.table + (size_t)b * g.max_pages;
+        const int cow = from >= 0 ? 1 : 0, have = pages_of(len, shift);
+        for (int i = lane; i < need - cow; i += 64) {
+            const int page = list[at + cow + i];
+            row[have + i] = page;
+            a.refs[page] = 1;
+        }
+        if (lane == 0) {
+            if (cow) {
+                const int page = list[at], m = atomicAdd(&s_moves, 1);
+                row[len >> shift] = page;
+                a.refs[page] = 1;
+                atomicSub(&a.refs[from], 1);
+                // (the copies are made in any order: no page is both read and written)
+                rows[kFrom * g.B + b] = -1;
+                rows[kTo * g.B + m] = b;
+                rows[kGroups * g.B + b] = ((len & in_page) + kGroup - 1) / kGroup;
+                rows[kNeed * g.B + b] = from;
+                rows[kAt * g.B + b] = page;
+            }
+            a.length[b] = len + n;
+            a.start[b] = len;
+        }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        a.ws[0] = s_moves;
+        const int status = s_status | (enough ? 0 : kStatusNoPages);
+        if (status) atomicOr(a.status, status);
+    }
+}
+
+// 16-byte pieces from one place to another by a workgroup
+__device__ __forceinline__ void copy_pieces(unsigned char *to, const unsigned char *from, size_t bytes)
+{
+    u32x4_t *y = reinterpret_cast<u32x4_t *>(to);
+    const u32x4_t *x = reinterpret_cast<const u32x4_t *>(from);
+    const int64_t n = (int64_t)(bytes / 16);
+    constexpr int U = 4;
+    for (int64_t i = threadIdx.x; i < n; i += 256 * U) {
+        u32x4_t v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + 256 * u < n) v[u] = x[i + 256 * u];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + 256 * u < n) {
+                y[i + 256 * u] = v[u];
+                hold_store_data(v[u]);
+            }
+    }
+}
+
+// the groups in use of every page that a row shared and goes on in
+__global__ __launch_bounds__(256) void reserve_copy_kernel(PagesArgs a)
+{
+    const PageGeom &g = a.g;
+    const int32_t *rows = a.ws + kHead;
+    const int64_t units = (int64_t)a.ws[0] * g.L * g.Hkv;
+    const size_t block = block_bytes(g);
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int h = (int)(u % g.Hkv), l = (int)(u / g.Hkv % g.L), b = rows[kTo * g.B + (int)(u / g.Hkv / g.L)];
+        const size_t from = rows[kNeed * g.B + b], to = rows[kAt * g.B + b], base = (size_t)l * g.n_pages;
+        copy_pieces(a.pool + ((base + to) * g.Hkv + h) * block, a.pool + ((base + from) * g.Hkv + h) * block,
+                    (size_t)rows[kGroups * g.B + b] * group_bytes(g.d));
+    }
+}
+
+// whether value v stands in x[0 .. n), asked by a whole workgroup
+__device__ __forceinline__ bool among(const int32_t *x, int n, int v)
+{
+    int hit = 0;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) hit |= x[i] == v;
+    return __syncthreads_or(hit);
+}
+
+// Row dst[i] becomes a second holder of row src[i]'s pages.
+__global__ __launch_bounds__(256) void fork_kernel(PagesArgs a)
+{
+    const PageGeom &g = a.g;
+    const int i = blockIdx.x, src = a.src[i], dst = a.dst[i];
+    // what is refused does not depend on the order of the pairs' workgroups: a row is written by the first pair that names it, and
+    // read by none that another pair writes
+    bool ok = (uint32_t)src < (uint32_t)g.B && (uint32_t)dst < (uint32_t)g.B;
+    ok = !among(a.dst, i, dst) && ok;
+    ok = !among(a.dst, a.n, src) && ok;
+    if (ok && a.length[dst] != 0) ok = false;
+    if (!ok) {
+        if (threadIdx.x == 0) atomicOr(a.status, kStatusPair);
+        return;
+    }
+    const int32_t *x = a.table + (size_t)src * g.max_pages;
+    int32_t *y = a.table + (size_t)dst * g.max_pages;
+    for (int j = threadIdx.x; j < g.max_pages; j += 256) {
+        const int page = x[j];
+        y[j] = page;
+        if ((uint32_t)page < (uint32_t)g.n_pages) atomicAdd(&a.refs[page], 1);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) a.length[dst] = a.length[src];
+}
+
+// Row rows[i] keeps tokens [first, keep) of what it holds: pages that lie wholly outside are given back.
+__global__ __launch_bounds__(256) void trim_kernel(PagesArgs a)
+{
+    const PageGeom &g = a.g;
+    const int i = blockIdx.x, b = a.src ? a.src[i] : i, shift = g.page_shift;
+    if ((uint32_t)b >= (uint32_t)g.B) return;
+    __shared__ int s_len;
+    if (threadIdx.x == 0) {
+        const int len = max(a.length[b], 0), keep = a.keep ? min(max(a.keep[i], 0), len) : len;
+        s_len = min(min(atomicMin(&a.length[b], keep), keep), g.max_pages << shift);
+    }
+    __syncthreads();
+    const int len = max(s_len, 0), first = a.first ? min(max(a.first[i], 0), len) : 0;
+    const int begin = first >> shift, end = pages_of(len, shift);
+    int32_t *row = a.table + (size_t)b * g.max_pages;
+    for (int j = threadIdx.x; j < g.max_pages; j += 256) {
+        if (j >= begin && j < end) continue;
+        if (row[j] < 0) continue;
+        const int page = atomicExch(&row[j], -1);              // (the row may be given twice: one of them takes the entry)
+        if ((uint32_t)page < (uint32_t)g.n_pages) atomicSub(&a.refs[page], 1);
+    }
+}
+
+// Page dst[i] becomes a copy of page src[i], all layers and heads.
+__global__ __launch_bounds__(256) void copy_kernel(PagesArgs a)
+{
+    const PageGeom &g = a.g;
+    const size_t block = block_bytes(g);
+    const int64_t units = (int64_t)a.n * g.L;
+    int last = -1;
+    bool ok = false;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int i = (int)(u / g.L), l = (int)(u - (int64_t)i * g.L), src = a.src[i], dst = a.dst[i];
+        if (i != last) {                   // (as in fork_kernel)
+            last = i;
+            ok = (uint32_t)src < (uint32_t)g.n_pages && (uint32_t)dst < (uint32_t)g.n_pages;
+            ok = !among(a.dst, i, dst) && ok;
+            ok = !among(a.dst, a.n, src) && ok;
+            if (!ok && threadIdx.x == 0) atomicOr(a.status, kStatusPair);
+        }
+        if (!ok) continue;
+        copy_pieces(a.pool + ((size_t)l * g.n_pages + dst) * g.Hkv * block, a.pool + ((size_t)l * g.n_pages + src) * g.Hkv * block, g.Hkv * block);
+    }
+}
+
+// The place of every page in use among those in use (or -1), and the counts in their new order; word 0 of the scratch: whether
+// they fit.
+__global__ __launch_bounds__(1024) void compact_rank_kernel(PagesArgs a)
+{
+    const PageGeom &g = a.g;
+    int32_t *rank = a.ws + kHead;
+    int used = 0;
+    constexpr int PER = 8;
+    for (int p0 = 0; p0 < g.n_pages; p0 += 1024 * PER) {
+        const int p = p0 + threadIdx.x * PER;
+        int bits = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (p + i < g.n_pages && a.refs[p + i] > 0) bits |= 1 << i;
+        int sum, at = block_scan<1024>(__popc(bits), sum);
+        at += used;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (p + i < g.n_pages) rank[p + i] = bits >> i & 1 ? at++ : -1;
+        used += sum;
+    }
+    __syncthreads();
+    const bool fits = used <= a.to_pages;
+    if (threadIdx.x == 0) {
+        a.ws[0] = fits;
+        if (!fits) atomicOr(a.status, kStatusNoPages);
+    }
+    if (!fits) return;
+    for (int p = threadIdx.x; p < g.n_pages; p += 1024)
+        if (rank[p] >= 0) a.to_refs[rank[p]] = a.refs[p];
+    for (int p = used + threadIdx.x; p < a.to_pages; p += 1024) a.to_refs[p] = 0;
+}
+
+__global__ __launch_bounds__(256) void compact_copy_kernel(PagesArgs a)
+{
+    if (!a.ws[0]) return;
+    const PageGeom &g = a.g;
+    const int32_t *rank = a.ws + kHead;
+    const size_t block = block_bytes(g);
+    const int64_t cells = (int64_t)g.B * g.max_pages, units = (int64_t)g.n_pages * g.L;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < cells; i += (int64_t)gridDim.x * 256) {
+        const int page = a.table[i];
+        a.to_table[i] = (uint32_t)page < (uint32_t)g.n_pages ? rank[page] : -1;
+    }
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int l = (int)(u / g.n_pages), p = (int)(u - (int64_t)l * g.n_pages), to = rank[p];
+        if (to < 0) continue;
+        copy_pieces(a.to_pool + ((size_t)l * a.to_pages + to) * g.Hkv * block, a.pool + ((size_t)l * g.n_pages + p) * g.Hkv * block, g.Hkv * block);
+    }
+}
+
+static unsigned grid_of(int64_t units, int64_t most) { return (unsigned)(units < 1 ? 1 : units < most ? units : most); }
+
+hipError_t launch_pages_reserve(const PagesArgs &a, hipStream_t st)
+{
+    hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(1024), 0, st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(reserve_copy_kernel, dim3(grid_of((int64_t)a.g.B * a.g.L * a.g.Hkv, 2048)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+hipError_t launch_pages_fork(const PagesArgs &a, hipStream_t st)
+{
+    hipLaunchKernelGGL(fork_kernel, dim3((unsigned)a.n), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+hipError_t launch_pages_trim(const PagesArgs &a, hipStream_t st)
+{
+    hipLaunchKernelGGL(trim_kernel, dim3((unsigned)a.n), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+hipError_t launch_pages_copy(const PagesArgs &a, hipStream_t st)
+{
+    hipLaunchKernelGGL(copy_kernel, dim3(grid_of((int64_t)a.n * a.g.L, 2048)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+hipError_t launch_pages_compact(const PagesArgs &a, hipStream_t st)
+{
+    hipLaunchKernelGGL(compact_rank_kernel, dim3(1), dim3(1024), 0, st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(compact_copy_kernel, dim3(grid_of((int64_t)a.g.n_pages * a.g.L, 2048)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace kvev

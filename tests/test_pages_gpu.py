@@ -1,0 +1,626 @@
+"""The paged 4-bit cache on the GPU: rows in and out, the page calls against a plain simulation, attention against 64 bits, and a
+run of them together."""
+import ctypes
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2509_21354_amd import binding as kb
+from tests import pages_ref as ref
+
+pytestmark = pytest.mark.gpu
+I32 = torch.int32
+
+
+def shape_of(L=1, B=1, H=4, H_kv=0, d=128, dtype=torch.bfloat16, T=0):
+    return kb.make_shape(L=L, B=B, H=H, H_kv=H_kv, d=d, T=T, T_cap=max(T, 1), C=1, N_cap=0, W=0, d_sum=1, d_g=1,
+                         dtype=kb.F32 if dtype == torch.float32 else kb.BF16)
+
+
+def ints(v):
+    return torch.tensor(v, dtype=I32, device="cuda")
+
+
+def normal(seed, *size, dtype=torch.bfloat16):
+    return torch.randn(size, generator=torch.Generator().manual_seed(seed)).to(dtype).cuda()
+
+
+def cache_of(sh, page, room, seed=0, spare=3, Tq=1, max_pages=None):
+    """A cache whose rows have pages for room[b] tokens, scattered over the pool."""
+    counts = [-(-n // page) for n in room]
+    c = kb.PagedCache(sh, page, sum(counts) + spare, max_pages or max(1, max(counts) + 1), Tq)
+    c.pool.random_(0, 256, generator=torch.Generator(device="cuda").manual_seed(seed))       # (NaN scales among the rest)
+    order = random.Random(seed).sample(range(c.pages.n_pages), c.pages.n_pages)
+    table = torch.full((sh.B, c.pages.max_pages), -1, dtype=I32)
+    for b, n in enumerate(counts):
+        table[b, :n] = torch.tensor([order.pop() for _ in range(n)], dtype=I32)
+    c.table.copy_(table)
+    c.refs.index_put_((table[table >= 0].long().cuda(),), torch.ones(sum(counts), dtype=I32, device="cuda"))
+    return c
+
+
+def fill(c, lengths, dtype, seed=1, K=None, V=None):
+    sh = c.shape
+    Tn = max(max(lengths), 1)
+    lead = (sh.L, sh.B, sh.H_kv or sh.H, Tn, sh.d)
+    K, V = normal(seed, *lead, dtype=dtype) if K is None else K, normal(seed + 1, *lead, dtype=dtype) if V is None else V
+    c.start.zero_()
+    c.length.copy_(ints(lengths))
+    c.append(K, V, Tn, c.length.clone())
+    return K, V
+
+
+# ---- rows in and out -------------------------------------------------------------------------------------------------------
+
+def edge_blocks(dtype):
+    """Blocks of 32 that try what rounding and scales can do, as [n, 32]."""
+    g = torch.Generator().manual_seed(3)
+    grid = torch.tensor([0.0, 0.25, 0.5, 0.75, 1.0, 1.25, 1.5, 1.75, 2.0, 2.5, 3.0, 3.5, 4.0, 5.0, 6.0, 7.0])
+    rows = [torch.cat((grid, -grid)), torch.zeros(32), -torch.zeros(32)]
+    near = torch.finfo(dtype).eps
+    for e in (-140, -132, -127, -126, -125, -124, -60, -1, 0, 1, 60, 120, 125):
+        rows.append(torch.cat((grid, -grid)).double().mul(2.0 ** e).float())
+        rows.append(torch.cat((grid * (1 + near), -grid * (1 - near / 2))).double().mul(2.0 ** e).float())
+    for top in (3.4e38, 3.0e38, 7.0, 7.0 * (1 + near), 7.0 * (1 - near / 2), 1e-45, 1e-38, 1e-40):
+        r = torch.randn(32, generator=g).clamp(-3, 3) / 4 * top
+        r[5] = top
+        rows.append(r)
+    for bad in (float("inf"), float("-inf"), float("nan")):
+        r = torch.randn(32, generator=g)
+        r[int(torch.randint(0, 32, (1,), generator=g))] = bad
+        rows.append(r)
+    rows += list(torch.randn(200, 32, generator=g) * 10.0 ** torch.randint(-38, 37, (200, 1), generator=g))
+    rows += list(torch.randn(100, 32, generator=g))
+    return torch.stack(rows).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_rounding_of_rows(dtype, d):
+    blocks = edge_blocks(dtype)
+    per = d // 32
+    n = blocks.shape[0] // per
+    x = blocks[:n * per].reshape(1, 1, 1, n, d).contiguous()
+    sh = shape_of(H=1, d=d, dtype=dtype)
+    c = cache_of(sh, 32, [n])
+    K, V = x.cuda(), x.flip(3).contiguous().cuda()
+    c.start.zero_()
+    c.append(K, V, n)
+    k, v = torch.empty_like(K), torch.empty_like(V)
+    c.read(c.start, None, n, k, v)
+    want = ref.cache_values(x)
+    for got, w in ((k, want), (v, want[:, :, :, ::-1])):
+        got = got.cpu().double().numpy()
+        assert np.array_equal(got, w, equal_nan=True), np.argwhere(~((got == w) | (np.isnan(got) & np.isnan(w))))[:5]
+        assert np.array_equal(np.signbit(got), np.signbit(w)) or np.isnan(w).any()
+
+
+def test_rounding_of_all_of_bf16():
+    """Every finite bf16 value beside a largest magnitude 0 to 4 powers of two above it."""
+    bits = torch.arange(0, 0x7F80, dtype=torch.int32)
+    v = (bits << 16).view(torch.float32)
+    tops = torch.stack([(v.double() * 2.0 ** k).clamp(max=3.38e38).float() for k in range(5)], 1).to(torch.bfloat16)      # [n, 5]
+    x = torch.zeros(bits.numel(), 5, 32, dtype=torch.bfloat16)
+    x[..., 0], x[..., 9] = v.to(torch.bfloat16)[:, None], tops
+    x[..., 17] = -v.to(torch.bfloat16)[:, None]
+    x = x.reshape(1, 1, 1, -1, 32)
+    n = x.numel() // 128
+    x = x.flatten()[:n * 128].reshape(1, 1, 1, n, 128).contiguous().cuda()
+    c = cache_of(shape_of(H=1), 256, [n])
+    c.start.zero_()
+    c.append(x, x, n)
+    k, w = torch.empty_like(x), torch.empty_like(x)
+    c.read(c.start, None, n, k, w)
+    # the same rule in torch, 64 bits
+    a = x.double().unflatten(-1, (-1, 32))
+    top = a.abs().amax(-1, keepdim=True)
+    m, e = torch.frexp(top)
+    e = torch.where(m > 0.875, e - 2, e - 3).clamp(-125, 125)             # top = m 2^e, m in [.5, 1): 7 = .875 * 2^3
+    y = (a * torch.exp2(-e.double())).abs()
+    step = torch.where(y < 2, 0.5, torch.where(y < 4, 1.0, 2.0))
+    want = ((torch.round(y / step) * step).clamp(max=6) * torch.exp2(e.double()) * torch.sign(a)).flatten(-2)
+    assert (torch.equal(k.double(), want) and torch.equal(w.double(), want)), (k.double() - want).abs().max()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("page,L,B,Hkv,d", [(16, 1, 1, 1, 64), (16, 2, 3, 2, 128), (64, 1, 4, 8, 128), (256, 2, 2, 3, 64)])
+def test_rows_land_where_they_belong(dtype, page, L, B, Hkv, d):
+    rng = random.Random(page + d)
+    cap = 3 * page + 5
+    start = [rng.randint(0, 2 * page) for _ in range(B)]
+    new = [rng.choice((0, 1, rng.randint(1, page), page + 3)) for _ in range(B)]
+    new[0] = max(new[0], 1)
+    Tn = page + 3
+    sh = shape_of(L=L, B=B, H=Hkv, d=d, dtype=dtype)
+    c = cache_of(sh, page, [cap] * B)
+    K, V = normal(5, L, B, Hkv, Tn, d, dtype=dtype), normal(6, L, B, Hkv, Tn, d, dtype=dtype)
+    k0, v0, k1, v1 = (torch.full((L, B, Hkv, cap, d), 9.0, dtype=dtype, device="cuda") for _ in range(4))
+    zero = ints([0] * B)
+    c.read(zero, None, cap, k0, v0)
+    before = c.pool.clone()
+    c.start.copy_(ints(start))
+    c.append(K, V, Tn, ints(new))
+    c.read(zero, None, cap, k1, v1)
+    kw, vw = torch.from_numpy(ref.cache_values(K)).cuda(), torch.from_numpy(ref.cache_values(V)).cuda()
+    for got, old, want in ((k1, k0, kw), (v1, v0, vw)):
+        expect = old.double()
+        for b in range(B):
+            expect[:, b, :, start[b]:start[b] + new[b]] = want[:, b, :, :new[b]]
+        assert torch.equal(torch.nan_to_num(got.double(), nan=1e300), torch.nan_to_num(expect, nan=1e300))
+    # nothing else in the pool moved: writing the same rows again changes nothing, undoing them gives the old pool
+    again = c.pool.clone()
+    c.append(K, V, Tn, ints(new))
+    assert torch.equal(again, c.pool)
+    changed = int((before != c.pool).sum())
+    assert changed <= L * Hkv * sum(new) * (d + d // 16)
+
+
+def test_rows_without_a_place():
+    """Negative starts, counts past the rows given, tokens past the capacity, entries that are no page."""
+    sh, page = shape_of(B=5, H=2), 16
+    c = cache_of(sh, page, [48] * 5, max_pages=3)
+    c.table[3, 1], c.table[4, 1] = c.pages.n_pages, -7
+    before = c.pool.clone()
+    K, V = normal(1, 1, 5, 2, 20, 128), normal(2, 1, 5, 2, 20, 128)
+    c.start.copy_(ints([-1, 40, 2 ** 31 - 1, 10, 10]))
+    c.append(K, V, 20, ints([20, 2 ** 31 - 1, 20, 20, 20]))
+    k, v = torch.full_like(K, 9.0), torch.full_like(V, 9.0)
+    c.read(c.start, ints([20, 25, 20, 20, 20]), 20, k, v)
+    want = torch.from_numpy(ref.cache_values(K)).cuda()
+    assert (k[:, 0] == 9).all() and (k[:, 2] == 9).all() and (v[:, 0] == 9).all()
+    assert torch.equal(k[:, 1, :, :8].double(), want[:, 1, :, :8]) and (k[:, 1, :, 8:] == 9).all()       # tokens 40 .. 47
+    for b in (3, 4):
+        assert torch.equal(k[:, b, :, :6].double(), want[:, b, :, :6]) and (k[:, b, :, 6:] == 0).all()
+    # pages of other rows are untouched
+    used = {int(c.table[1, 2])} | {int(c.table[b, 0]) for b in (3, 4)}
+    pool, old = c.pool.view(c.pages.n_pages, -1), before.view(c.pages.n_pages, -1)
+    for p in range(c.pages.n_pages):
+        assert p in used or torch.equal(pool[p], old[p]), p
+    c.append(K, V, 0)
+    c.read(c.start, None, 0, k, v)
+
+
+# ---- attention -------------------------------------------------------------------------------------------------------------
+
+def check_attention(c, Q, O, lengths, first=None, q_start=None, store=None, heads=None, what=""):
+    """Against 64 bits on the values that the cache holds; heads: which (layer, row, key-value head) to look at."""
+    sh = c.shape
+    L, B, H, Hkv, d, Tq = sh.L, sh.B, sh.H, sh.H_kv or sh.H, sh.d, Q.shape[3]
+    G, dtype = H // Hkv, Q.dtype
+    Tm = max(max(lengths), 1)
+    k, v = (torch.zeros(L, B, Hkv, Tm, d, dtype=dtype, device="cuda") for _ in range(2))
+    c.read(ints([0] * B), None, min(Tm, c.pages.max_pages * c.pages.page), k, v)
+    k, v, q, o = (x.cpu().double().numpy() for x in (k, v, Q, O))
+    table = c.table.cpu().numpy()
+    for l, b, h in heads or [(l, b, h) for l in range(L) for b in range(B) for h in range(Hkv)]:
+        n = lengths[b]
+        t = np.arange(n)
+        page = table[b, t // c.pages.page] if n else np.zeros(0, int)
+        there = (page >= 0) & (page < c.pages.n_pages) & (t >= (first[b] if first else 0))
+        vis = np.broadcast_to(there, (G, Tq, n)).copy()
+        if q_start is not None:
+            vis &= t[None, None, :] <= (q_start[b] + np.arange(Tq))[None, :, None]
+        K, V = k[l, b, h, :n], v[l, b, h, :n]
+        m = 0
+        if store:
+            m = int(store[2][l, b, h])
+            K, V = np.concatenate((store[0][l, b, h, :m].cpu().double().numpy(), K)), np.concatenate((store[1][l, b, h, :m].cpu().double().numpy(), V))
+            vis = np.concatenate((np.ones((G, Tq, m), bool), vis), 2)
+        want, E, S = ref.attention(q[l, b, h * G:(h + 1) * G].reshape(G * Tq, d), K, V, vis.reshape(G * Tq, -1), 1 / np.sqrt(d))
+        got = o[l, b, h * G:(h + 1) * G].reshape(G * Tq, d)
+        bound = ref.attention_bound(want, E, S, n + m, d, dtype, G * Tq > 16)
+        bad = ~(np.abs(got - want) <= bound)
+        assert not bad.any(), (what, (l, b, h), np.argwhere(bad)[:4], got[bad][:4], want[bad][:4], bound[bad][:4])
+
+
+CASES = [  # dtype, d, page, L, B, H, Hkv, lengths, Tq, causal, k_cap
+    ("bf16", 128, 16, 1, 1, 1, 1, [1], 1, False, 0),
+    ("f32", 64, 16, 1, 1, 1, 1, [1], 1, False, 0),
+    ("bf16", 128, 32, 1, 4, 4, 4, [0, 1, 33, 200], 1, False, 0),
+    ("bf16", 128, 64, 2, 3, 8, 2, [63, 64, 65], 1, False, 0),
+    ("f32", 128, 16, 1, 3, 8, 2, [17, 300, 129], 1, False, 0),
+    ("bf16", 64, 256, 1, 2, 16, 1, [700, 1], 1, False, 0),
+    ("bf16", 128, 64, 1, 2, 8, 8, [2100, 5], 1, False, 0),
+    ("f32", 64, 128, 1, 2, 2, 1, [1500, 640], 1, True, 0),
+    ("bf16", 128, 16, 1, 3, 4, 2, [40, 7, 300], 5, True, 0),
+    ("bf16", 128, 32, 1, 2, 4, 2, [130, 131], 8, True, 0),
+    ("bf16", 128, 32, 1, 2, 4, 4, [260, 90], 17, True, 0),
+    ("bf16", 64, 64, 1, 2, 4, 1, [500, 100], 33, True, 0),
+    ("bf16", 128, 64, 2, 1, 8, 2, [333], 100, False, 0),
+    ("f32", 128, 32, 1, 2, 4, 4, [150, 64], 20, True, 0),
+    ("f32", 64, 16, 1, 2, 4, 2, [100, 31], 33, True, 20),
+    ("bf16", 128, 64, 1, 3, 4, 2, [100, 0, 64], 1, False, 70),
+    ("f32", 128, 64, 1, 2, 4, 4, [90, 0], 3, False, 5),
+    ("bf16", 64, 32, 2, 2, 4, 2, [0, 45], 40, False, 130),
+    ("bf16", 128, 128, 1, 1, 4, 2, [1000], 150, True, 17),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c)).replace(" ", ""))
+def test_attention(case):
+    name, d, page, L, B, H, Hkv, lengths, Tq, causal, k_cap = case
+    dtype = torch.float32 if name == "f32" else torch.bfloat16
+    for T in {0, max(lengths), 1}:
+        sh = shape_of(L, B, H, Hkv, d, dtype, T)
+        c = cache_of(sh, page, lengths, Tq=Tq)
+        fill(c, lengths, dtype)
+        Q = normal(7, L, B, H, Tq, d, dtype=dtype)
+        O = torch.full_like(Q, 9.0)
+        store = None
+        if k_cap:
+            count = torch.randint(0, k_cap + 1, (L, B, Hkv), generator=torch.Generator().manual_seed(2))
+            count.view(-1)[0], count.view(-1)[-1] = 0, k_cap
+            store = (normal(8, L, B, Hkv, k_cap, d, dtype=dtype), normal(9, L, B, Hkv, k_cap, d, dtype=dtype), count.to(I32).cuda())
+        # a frame of tokens at the end of each row; in short rows the first of them lie before it and see nothing
+        q_start = [n - Tq for n in lengths] if causal else None
+        kb.kvev_page_attention(sh, c.pages, Q, Tq, c.pool, c.table, c.length, O, c.ws_attn, None, ints(q_start) if causal else None,
+                               *(store or (None, None, None)), k_cap)
+        check_attention(c, Q, O, lengths, None, q_start, store, what=f"T={T}")
+        again = torch.full_like(Q, -9.0)
+        kb.kvev_page_attention(sh, c.pages, Q, Tq, c.pool, c.table, c.length, again, c.ws_attn, None, ints(q_start) if causal else None,
+                               *(store or (None, None, None)), k_cap)
+        assert torch.equal(O, again)                     # the same bits, and the tickets are zero again
+        head = c.ws_attn[:4 * L * B * Hkv]
+        assert not head.any()
+
+
+@pytest.mark.parametrize("Tq", [1, 40])
+def test_attention_over_a_window(Tq):
+    """Tokens before `first` and pages given up; entries that are no page inside the window; lengths that are wrong."""
+    sh, lengths, first = shape_of(B=4, H=4, H_kv=2), [300, 200, 150, 90], [100, 64, 149, 90]
+    c = cache_of(sh, 32, lengths[:3] + [96], Tq=Tq)
+    fill(c, lengths[:3] + [96], torch.bfloat16)
+    c.length[3] = 90
+    c.table[0, :3] = -1
+    c.table[1, 4] = c.pages.n_pages + 3
+    Q = normal(7, 1, 4, 4, Tq, 128)
+    O = torch.empty_like(Q)
+    kb.kvev_page_attention(sh, c.pages, Q, Tq, c.pool, c.table, c.length, O, c.ws_attn, ints(first))
+    check_attention(c, Q, O, lengths, first)
+    assert (O[:, 3] == 0).all()
+    for wrong, right in ((-5, 0), (2 ** 31 - 1, c.pages.max_pages * 32)):
+        c.length[3] = wrong
+        kb.kvev_page_attention(sh, c.pages, Q, Tq, c.pool, c.table, c.length, O, c.ws_attn, ints([0, 0, 0, -3]))
+        check_attention(c, Q, O, lengths[:3] + [right])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("Tq", [1, 30])
+def test_attention_keeps_what_is_hidden_apart(dtype, Tq):
+    """Blocks that are not finite: in hidden tokens they change nothing, in seen ones a key spoils the query, a value its block."""
+    n = 150
+    sh = shape_of(B=2, H=4, H_kv=2, dtype=dtype)
+    K, V = normal(1, 1, 2, 2, n, 128, dtype=dtype), normal(2, 1, 2, 2, n, 128, dtype=dtype)
+    K2, V2 = K.clone(), V.clone()
+    K2[:, 0, :, 140, 3], V2[:, 0, :, 141, 70] = float("nan"), float("inf")       # row 0: behind what its queries see
+    V2[:, 1, 0, 20, 100] = float("nan")                                          # row 1, head 0: in sight; block 3
+    K2[:, 1, 1, 30, 0] = float("-inf")                                           # row 1, head 1: every query
+    out = []
+    for k, v in ((K, V), (K2, V2)):
+        c = cache_of(sh, 64, [n, n], Tq=Tq)
+        fill(c, [n, n], dtype, K=k, V=v)
+        Q = normal(7, 1, 2, 4, Tq, 128, dtype=dtype)
+        O = torch.empty_like(Q)
+        kb.kvev_page_attention(sh, c.pages, Q, Tq, c.pool, c.table, c.length, O, c.ws_attn, None, ints([100, n - Tq]))
+        out.append(O)
+    clean, O = out
+    assert torch.equal(O[:, 0], clean[:, 0])
+    assert torch.isnan(O[:, 1, 0:2, :, 96:]).all() and torch.equal(O[:, 1, 0:2, :, :96], clean[:, 1, 0:2, :, :96])
+    assert torch.isnan(O[:, 1, 2:4]).all()
+
+
+def test_attention_scores_of_every_size():
+    """Keys and queries so large that all weight is on one token, and so small that it is shared alike."""
+    sh, n = shape_of(B=2, H=2, dtype=torch.float32), 200
+    for scale in (1e-20, 30.0, 1e15):
+        K = normal(1, 1, 2, 2, n, 128, dtype=torch.float32) * scale
+        c = cache_of(sh, 16, [n, n])
+        fill(c, [n, n], torch.float32, K=K)
+        Q = normal(3, 1, 2, 2, 1, 128, dtype=torch.float32)
+        O = torch.empty_like(Q)
+        c.attend(Q, 1, O)
+        assert torch.isfinite(O).all()
+        if scale < 1e10:
+            check_attention(c, Q, O, [n, n])
+        else:                                    # all weight on one token: scores are 1e12 and more apart
+            k, v = torch.empty_like(K), torch.empty_like(K)
+            c.read(ints([0, 0]), None, n, k, v)
+            best = torch.matmul(k.double(), Q.double().transpose(3, 4).contiguous()).squeeze(-1).argmax(-1)
+            assert torch.equal(O[..., 0, :], torch.gather(v, 3, best[..., None, None].expand(-1, -1, -1, 1, 128)).squeeze(3))
+
+
+def test_attention_of_a_long_cache():
+    """A pool of more than 2^32 bytes, whose last pages lie behind them: 2 layers, both ends of it read."""
+    sh = shape_of(L=2, B=1, H=8, d=128, T=1 << 18)
+    page, n_pages = 256, 9000                                                   # 2 x 9000 x 8 x 34 816 bytes
+    c = kb.PagedCache(sh, page, n_pages, 1024)
+    assert c.pool.numel() > 5 * 10 ** 9
+    lengths = [200 * 256 + 77]
+    order = list(range(n_pages - 1, n_pages - 102, -1)) + list(range(100))
+    c.table[0, :201] = ints(order)
+    K, V = normal(1, 2, 1, 8, lengths[0], 128), normal(2, 2, 1, 8, lengths[0], 128)
+    c.length.copy_(ints(lengths))
+    c.append(K, V, lengths[0])
+    Q = normal(3, 2, 1, 8, 1, 128) * 3
+    O = torch.empty_like(Q)
+    c.attend(Q, 1, O)
+    check_attention(c, Q, O, lengths, heads=[(0, 0, 0), (1, 0, 7)])
+
+
+# ---- page calls ------------------------------------------------------------------------------------------------------------
+
+def same_state(c, sim):
+    assert c.length.tolist() == sim.length and c.refs.tolist() == sim.refs and c.table.tolist() == sim.table
+    assert int(c.status) == sim.status
+    held = [0] * len(sim.refs)
+    for row in sim.table:
+        for p in row:
+            if p >= 0:
+                held[p] += 1
+    assert held == sim.refs
+
+
+@pytest.mark.parametrize("B,page,n_pages,max_pages,seed", [(1, 16, 5, 4, 0), (5, 16, 40, 9, 1), (7, 32, 30, 6, 2), (33, 64, 150, 5, 3), (1100, 16, 9000, 12, 4)])
+def test_page_calls_against_a_plain_simulation(B, page, n_pages, max_pages, seed):
+    rng = random.Random(seed)
+    sh = shape_of(L=2, B=B, H=2, d=64)
+    c, sim = kb.PagedCache(sh, page, n_pages, max_pages), ref.Sim(B, page, n_pages, max_pages)
+    c.pool.random_(0, 256)
+    for step in range(12 if B > 100 else 40):
+        what = rng.choice(("reserve", "reserve", "reserve", "fork", "trim", "trim"))
+        if what == "reserve":
+            n = [rng.choice((0, 0, 1, 1, rng.randint(0, 2 * page), -3, max_pages * page if rng.random() < 0.05 else 2)) for _ in range(B)]
+            before = c.pool.clone().view(2, n_pages, 2, page // 16, -1)
+            c.reserve(ints(n))
+            starts, copies = sim.reserve(n)
+            assert c.start.tolist() == starts
+            after = c.pool.view(2, n_pages, 2, page // 16, -1)
+            want = before.clone()
+            for a, b, tokens in copies:
+                g = -(-tokens // 16)
+                want[:, b, :, :g] = before[:, a, :, :g]
+            assert torch.equal(after, want)
+        elif what == "fork":
+            n = rng.randint(1, max(1, B // 2))
+            src, dst = [rng.randint(-1, B) if rng.random() < 0.1 else rng.randrange(B) for _ in range(n)], [rng.randrange(B) for _ in range(n)]
+            c.fork(ints(src), ints(dst), n)
+            sim.fork(src, dst)
+        else:
+            n = rng.randint(1, B)
+            rows = None if rng.random() < 0.3 else [rng.randint(-1, B) if rng.random() < 0.1 else x for x in rng.sample(range(B), n)]
+            first = [rng.choice((0, 0, rng.randint(-2, max_pages * page))) for _ in range(n)] if rng.random() < 0.6 else None
+            keep = [rng.choice((0, -1, rng.randint(0, max_pages * page))) for _ in range(n)] if rng.random() < 0.6 else None
+            c.trim(None if rows is None else ints(rows), n, None if first is None else ints(first), None if keep is None else ints(keep))
+            sim.trim(range(n) if rows is None else rows, first, keep)
+        same_state(c, sim)
+
+
+def test_reserve_refusals():
+    sh = shape_of(B=3, H=1, d=64)
+    c, sim = kb.PagedCache(sh, 16, 4, 3), ref.Sim(3, 16, 4, 3)
+    for n in ([17, 16, 2 ** 31 - 1], [40, 1, 0], [0, 16, 0], [16, 1, 1]):          # past the capacity; too few pages; the last ones
+        c.reserve(ints(n))
+        assert c.start.tolist() == sim.reserve(n)[0]
+        same_state(c, sim)
+    c.table[0, 1] = -1                                       # the page that row 0 would go on in is missing
+    c.refs[1] -= 1
+    c.length[0] = 20
+    c.reserve(ints([1, 0, 0]))
+    assert c.start.tolist()[0] == -1 and int(c.length[0]) == 20 and int(c.status) & kb.PAGES_BAD_ROW
+
+
+def test_trim_of_a_row_given_twice():
+    sh = shape_of(B=2, H=1, d=64)
+    c = kb.PagedCache(sh, 16, 8, 4)
+    c.reserve(ints([60, 20]))
+    c.trim(ints([0, 0]), 2, None, ints([40, 17]))
+    assert c.length.tolist() == [17, 20] and c.refs.tolist() == [1, 1, 0, 0, 1, 1, 0, 0]
+    assert c.table.tolist() == [[0, 1, -1, -1], [4, 5, -1, -1]]
+
+
+def test_copy_of_pages():
+    sh = shape_of(L=3, B=1, H=2, d=128)
+    c = kb.PagedCache(sh, 32, 12, 2)
+    c.pool.random_(0, 256)
+    before = c.pool.clone().view(3, 12, -1)
+    # the second pair with destination 7, a chain (4 is written), places outside, a page onto itself: refused
+    src, dst = [0, 1, 4, 2, -1, 12, 3, 10], [7, 7, 8, 4, 5, 6, 12, 10]
+    kb.kvev_pages_copy(sh, c.pages, c.pool, ints(src), ints(dst), 8, c.status)
+    want = before.clone()
+    want[:, 7], want[:, 4] = before[:, 0], before[:, 2]
+    assert torch.equal(c.pool.view(3, 12, -1), want) and int(c.status) == kb.PAGES_BAD_PAIR
+
+
+@pytest.mark.parametrize("n_pages,max_pages,B,page", [(5, 2, 1, 16), (300, 9, 11, 32), (20000, 40, 300, 16)])
+def test_compact(n_pages, max_pages, B, page):
+    rng = random.Random(n_pages)
+    sh = shape_of(L=2, B=B, H=1, d=64)
+    c = kb.PagedCache(sh, page, n_pages, max_pages)
+    c.pool.random_(0, 256)
+    table = torch.full((B, max_pages), -1, dtype=I32)
+    order = rng.sample(range(n_pages), min(n_pages, B * max_pages))
+    refs = torch.zeros(n_pages, dtype=I32)
+    for b in range(B):
+        for j in range(rng.randint(0, max_pages)):
+            table[b, j] = order[b * max_pages + j] if b * max_pages + j < len(order) and rng.random() < 0.8 else rng.choice(order)
+            refs[table[b, j]] += 1
+    c.table.copy_(table)
+    c.refs.copy_(refs)
+    live = [p for p in range(n_pages) if refs[p] > 0]
+    for room in {len(live) - 1, len(live), len(live) + 3} - {0, -1}:
+        t = kb.PagedCache(sh, page, room, max_pages)
+        t.pool.fill_(77)
+        t.table.fill_(-5)
+        t.refs.fill_(-5)
+        ws = kb.alloc_workspace(kb.page_workspace_bytes(kb.OP_PAGES_COMPACT, sh, c.pages, 0))
+        kb.kvev_pages_compact(sh, c.pages, c.pool, c.table, c.refs, t.pages, t.pool, t.table, t.refs, t.status, ws)
+        if room < len(live):
+            assert int(t.status) == kb.PAGES_NONE_FREE and (t.pool == 77).all() and (t.table == -5).all() and (t.refs == -5).all()
+            continue
+        rank = {p: i for i, p in enumerate(live)}
+        assert int(t.status) == 0 and t.refs.tolist() == [int(refs[p]) for p in live] + [0] * (room - len(live))
+        assert t.table.tolist() == [[rank.get(int(p), -1) for p in row] for row in table]
+        x, y = c.pool.view(2, n_pages, -1), t.pool.view(2, room, -1)
+        assert torch.equal(y[:, :len(live)], x[:, torch.tensor(live, device="cuda")]) and (y[:, len(live):] == 77).all()
+
+
+# ---- together --------------------------------------------------------------------------------------------------------------
+
+def raw_attention(Q, K, V, n, Tq, causal):
+    """float64, contiguous rows"""
+    H, Hkv, d = Q.shape[2], K.shape[2], Q.shape[4]
+    k, v = (x[..., :n, :].double().repeat_interleave(H // Hkv, 2) for x in (K, V))
+    s = torch.matmul(Q.double(), k.transpose(3, 4).contiguous()) / d ** 0.5
+    if causal:
+        s = s.masked_fill(torch.arange(n, device=s.device) > (n - Tq + torch.arange(Tq, device=s.device))[:, None], float("-inf"))
+    return torch.matmul(torch.softmax(s, -1), v)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_frames_forks_eviction_and_summaries_together(dtype):
+    """Two frames of tokens with rotary positions, a fork, tokens that go apart, chunks pooled from the pages and the window moved on."""
+    L, B, H, Hkv, d, page, Tf = 2, 3, 4, 2, 64, 16, 50
+    sh = shape_of(L, B, H, Hkv, d, dtype)
+    c = kb.PagedCache(sh, page, 40, 10, Tf)
+    axes, freq = kb.make_rotary_axes((8, 12, 12)), (10000.0 ** (-torch.arange(32) / 32.0)).cuda()
+    raw = [[torch.zeros(L, Hkv, 0, d, dtype=torch.float64, device="cuda") for _ in range(B)] for _ in range(2)]
+    held = [0] * B
+
+    def step(seed, n_new, Tn):
+        Q, K, V = (normal(seed + i, L, B, h, Tn, d, dtype=dtype) for i, h in enumerate((H, Hkv, Hkv)))
+        pos = torch.stack([torch.stack([torch.full((Tn,), held[b]), torch.arange(Tn) // 8, torch.arange(Tn) % 8]) for b in range(B)], 1).to(I32).cuda()
+        kb.kvev_rotary(sh, axes, freq, pos, Tn, Q, K, Q, K)                     # in place
+        c.reserve(ints(n_new))
+        c.append(K, V, Tn, ints(n_new))
+        for b in range(B):
+            for i, x in enumerate((K, V)):
+                raw[i][b] = torch.cat((raw[i][b], torch.from_numpy(ref.cache_values(x[:, b, :, :n_new[b]])).cuda()), 2)
+            held[b] += n_new[b]
+        O = torch.empty_like(Q)
+        c.attend(Q, Tn, O, causal=True)
+        for b in range(B):
+            n = n_new[b]
+            if n:
+                want = raw_attention(Q[:, b:b + 1, :, :n], raw[0][b][:, None], raw[1][b][:, None], held[b], n, True)
+                err = (O[:, b:b + 1, :, :n].double() - want).abs().max()
+                # values of N(0, 1) rows and weights that sum to 1: |O| and the sum of weights times |V| stay below 6 (largest value held)
+                assert err <= 6 * (2.0 ** -8 * 3 if dtype == torch.bfloat16 else 2.0 ** -15), (seed, b, err)
+        assert c.length.tolist() == held and int(c.status) == 0
+
+    step(10, [50, 31, 0], 50)
+    step(20, [33, 50, 0], 50)
+    c.fork(ints([0]), ints([2]), 1)
+    held[2] = held[0]
+    for i in range(2):
+        raw[i][2] = raw[i][0].clone()
+    step(30, [1, 1, 1], 1)                   # rows 0 and 2 go on apart from one page
+    step(40, [7, 0, 20], 20)
+    # chunks of 16 tokens of row 1, out of the pages and through the library's pooling
+    K, V = (torch.empty(L, B, Hkv, 64, d, dtype=dtype, device="cuda") for _ in range(2))
+    c.read(ints([0] * B), None, 64, K, V)
+    Kb, Vb = torch.empty(L, B, Hkv, 4, d, dtype=dtype, device="cuda"), torch.empty(L, B, Hkv, 4, d, dtype=dtype, device="cuda")
+    psh = kb.make_shape(L=L, B=B, H=H, H_kv=Hkv, d=d, T=64, T_cap=64, C=16, N_cap=4, W=0, d_sum=32, d_g=64, dtype=sh.dtype)
+    kb.kvev_chunk_pool(psh, K, V, kb.POOL_MEAN, None, None, 0, 4, Kb, Vb)
+    want = raw[0][1][:, :, :64].reshape(L, Hkv, 4, 16, d).mean(3)
+    assert (Kb[:, 1].double() - want).abs().max() <= 8 * 2.0 ** -8 and int(c.length[1]) == held[1]
+    # the window moves past those chunks, whose summaries take their place
+    free = int((c.refs == 0).sum())
+    first = ints([64] * B)
+    c.trim(None, B, first)
+    assert int((c.refs == 0).sum()) >= free + 8
+    Q = normal(50, L, B, H, 1, d, dtype=dtype)
+    O = torch.empty_like(Q)
+    count = torch.full((L, B, Hkv), 4, dtype=I32, device="cuda")
+    c.attend(Q, 1, O, first, False, Kb, Vb, count, 4)
+    check_attention(c, Q, O, held, [64] * B, None, (Kb, Vb, count))
+    c.trim(None, B, None, ints([0] * B))
+    assert not c.refs.any() and not c.length.any() and (c.table == -1).all()
+
+
+def test_a_decode_step_in_a_graph():
+    """rotary, reserve, append, attention captured once and replayed as the cache grows; two graphs share a workspace."""
+    L, B, H, d, page, N = 1, 3, 4, 128, 16, 40
+    sh = shape_of(L, B, H, 2, d)
+    axes, freq = kb.make_rotary_axes((64,)), (10000.0 ** (-torch.arange(64) / 64.0)).cuda()
+    Qs, Ks, Vs = (normal(i, N, L, B, h, 1, d) for i, h in enumerate((H, 2, 2)))
+
+    def run(graphs):
+        c = kb.PagedCache(sh, page, 30, 6)
+        Q, K, V, O = Qs[0].clone(), Ks[0].clone(), Vs[0].clone(), torch.empty_like(Qs[0])
+        one, outs = ints([1, 1, 0]), []
+
+        def step():
+            kb.kvev_rotary(sh, axes, freq, c.length, 1, Q, K, Q, K)       # position: the length before
+            c.reserve(one)
+            c.append(K, V, 1, one)
+            c.attend(Q, 1, O, causal=True)
+        captured = []
+        if graphs:
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                kb.kvev_page_attention(sh, c.pages, Q, 1, c.pool, c.table, c.length, O, c.ws_attn)      # (loads the kernels)
+            torch.cuda.current_stream().wait_stream(side)
+            for _ in range(2):
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g):
+                    step()
+                captured.append(g)
+        for i in range(N):
+            for x, y in ((Q, Qs), (K, Ks), (V, Vs)):
+                x.copy_(y[i])
+            captured[i % 2].replay() if graphs else step()
+            outs.append(O.clone())
+            if i % 7 == 0:
+                torch.cuda.synchronize()
+        assert c.length.tolist() == [N, N, 0] and int(c.status) == 0
+        return torch.stack(outs)
+    assert torch.equal(run(False), run(True))
+
+
+def test_calls_on_another_stream():
+    sh = shape_of(B=2, H=4, H_kv=2)
+    c = cache_of(sh, 32, [200, 90])
+    fill(c, [200, 90], torch.bfloat16)
+    Q = normal(7, 1, 2, 4, 1, 128)
+    O, P = torch.empty_like(Q), torch.empty_like(Q)
+    c.attend(Q, 1, O)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        c.attend(Q, 1, P)
+    s.synchronize()
+    assert torch.equal(O, P)
+
+
+def test_python_calls_by_either_way(monkeypatch):
+    """The extension module and ctypes lead to the same call."""
+    sh = shape_of(B=2, H=4, H_kv=2)
+    outs = []
+    for native in (kb._native, None):
+        monkeypatch.setattr(kb, "_native", native)
+        c = kb.PagedCache(sh, 32, 20, 8)
+        c.reserve(ints([70, 33]))
+        K, V, Q = normal(1, 1, 2, 2, 70, 128), normal(2, 1, 2, 2, 70, 128), normal(3, 1, 2, 4, 1, 128)
+        kb.kvev_rotary(sh, kb.make_rotary_axes((32, 32)), torch.ones(64, device="cuda"), ints([[[3] * 70] * 2] * 2), 70, None, K, None, K)
+        c.append(K, V, 70, ints([70, 33]))
+        c.trim(ints([1]), 1, ints([0]), ints([20]))
+        c.reserve(ints([0, 5]))
+        O, k, v = torch.empty_like(Q), torch.zeros_like(K), torch.zeros_like(V)
+        c.attend(Q, 1, O, ints([0, 3]), True)
+        c.read(ints([1, 1]), ints([60, 20]), 70, k, v)
+        c.trim(None, 2, None, ints([0, 30]))
+        c.fork(ints([1]), ints([0]), 1)
+        outs.append([O, k, v, c.table.clone(), c.length.clone(), c.refs.clone(), c.status.clone()])
+        with pytest.raises(kb.KvevError, match="table has to hold 16 elements of torch.int32"):
+            kb.kvev_page_append(sh, c.pages, K, V, 70, c.start, None, c.table.long(), c.pool)
+        with pytest.raises(kb.KvevError, match="length is not on the current device"):
+            kb.kvev_page_attention(sh, c.pages, Q, 1, c.pool, c.table, c.length.cpu(), O, c.ws_attn)
+        with pytest.raises(kb.KvevError, match="workspace"):
+            kb.kvev_pages_reserve(sh, c.pages, ints([1, 1]), c.table, c.length, c.refs, c.pool, c.start, c.status, None)
+        with pytest.raises(AssertionError, match="contiguous"):
+            kb.kvev_page_append(sh, c.pages, K, V.transpose(2, 3).contiguous().transpose(2, 3), 70, c.start, None, c.table, c.pool)
+    for x, y in zip(*outs):
+        assert torch.equal(x, y)
