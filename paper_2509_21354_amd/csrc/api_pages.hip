@@ -194,6 +194,7 @@ int kvev_page_attention(const kvev_shape *sh, const kvev_pages *pg, const void *
         a.tickets = static_cast<int32_t *>(ws);
         a.part = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + p.ticket_bytes);
     }
+    a.stream = (size_t)sh->L * sh->B * a.g.Hkv * (size_t)plan_tokens(sh, a.g) * 17 * sh->d / 16 > kCacheBytes;
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)sh->d));
     const hipError_t e = launch_page_attention(a, sh->dtype, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? KVEV_OK : hip_fail(e);

@@ -95,17 +95,29 @@ template <int D> __device__ __forceinline__ int lane_offset(int n, int gr) { ret
 template <int D> struct Codes;            // a lane's quarter of a token's codes
 template <> struct Codes<128> { typedef u32x4_t type; };
 template <> struct Codes<64> { typedef u32x2_t type; };
+// from a base that is the same in all lanes
+template <bool STREAM, typename V> __device__ __forceinline__ V load_codes(const unsigned char *base, uint32_t offset)
+{
+    const V *p = reinterpret_cast<const V *>(base + offset);
+    return STREAM ? __builtin_nontemporal_load(p) : *p;
+}
 #endif
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void page_attention_kernel(PageAttnArgs a)
+// A wave's staging rows: 32 tokens, unpadded.  Piece p (16 bytes) of token t lies at p ^ turn(t): the 16-byte writes of 16 tokens'
+// piece p and the transposing reads of 8 tokens' neighbouring pieces then touch every bank once.
+template <int D> __device__ __forceinline__ int turn_of(int t)
+{
+    return D == 128 ? (t & 7) << 1 | (t >> 3 & 1) : (t >> 1 & 3) << 1 | (t >> 3 & 1);
+}
+
+template <typename T, int D, bool STREAM>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_kernel(PageAttnArgs a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int NQ = Terms<T>::Q, NP = Terms<T>::P, KS = D / 32, DT = D / 16, NB = D / 32;
-    constexpr int RPV = D + 16;                  // pitch of the staged values (see the frame kernels)
     constexpr int OP = D + 4;                    // pitch of the waves' outputs
-    constexpr int STAGE = 32 * RPV * 2, OUT = 16 * OP * 4;
-    __shared__ __align__(16) unsigned char s_mem[4 * (STAGE > OUT ? STAGE : OUT)];
+    constexpr int STAGE = 32 * D * 2, OUT = 16 * OP * 4;
+    __shared__ __align__(256) unsigned char s_mem[4 * (STAGE > OUT ? STAGE : OUT)];
     __shared__ float s_m[4][16], s_l[4][16];
 
     const PageGeom &g = a.g;
@@ -128,8 +140,14 @@ __global__ __launch_bounds__(256) void page_attention_kernel(PageAttnArgs a)
     // this lane's query, and the last token that it sees
     const int r = qt * 16 + n, rc = min(r, R - 1), gq = rc / a.Tq, tq = rc - gq * a.Tq;
     const size_t orow = (((size_t)lb * g.Hkv + h) * a.G + gq) * a.Tq + tq;
-    int lim = len - 1;
-    if (a.q_start) lim = (int)min<int64_t>(lim, (int64_t)a.q_start[b] + tq);
+    int lim = len - 1, lim_all = len - 1;        // ... and the last one that all of the unit's queries see
+    if (a.q_start) {
+        const int64_t at = a.q_start[b];
+        lim = (int)min<int64_t>(lim, at + tq);
+        // (a unit whose queries are the ends of two heads and the beginning of a third has token 0 among them)
+        const int t0 = qt * 16 / a.Tq == min(qt * 16 + 15, R - 1) / a.Tq ? qt * 16 % a.Tq : 0;
+        lim_all = (int)min<int64_t>(lim_all, at + t0);
+    }
     bf16x8_t qf[KS][NQ];
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) Terms<T>::load(static_cast<const T *>(a.Q) + orow * D + gr * (D / 4) + kk * 8, qf[kk]);
@@ -140,20 +158,26 @@ __global__ __launch_bounds__(256) void page_attention_kernel(PageAttnArgs a)
     for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     uint32_t nan_blocks = 0;                     // blocks of d whose values are NaN in a token that query n sees
 
-    bf16_t *s_v = reinterpret_cast<bf16_t *>(s_mem + wave * STAGE);
+    // staging: lane (n, gr) writes pieces gr * KS + kk of tokens n and 16 + n; it reads, of tokens 4 gr + n / 4 and 16 further on, piece
+    // 2 dt + (n & 3) / 2, half n & 1
+    unsigned char *s_v = s_mem + wave * STAGE;
+    unsigned char *put[KS];
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) put[kk] = s_v + n * (2 * D) + (((gr * KS + kk) ^ turn_of<D>(n)) << 4);
+    const int row = 4 * gr + (n >> 2);
+    const uint32_t get = (uint32_t)(row * (2 * D) + ((((n & 3) >> 1) ^ turn_of<D>(row)) << 4) + (n & 1) * 8);
+
     const float c = a.scale_log2e;
     const size_t block = block_bytes(g);
     const unsigned char *pool = a.pool + ((size_t)l * g.n_pages * g.Hkv + h) * block;
-    const int32_t *table = a.table + (size_t)b * g.max_pages;
 
     // the weights of a chunk from its scores (hidden ones: -inf), and the running state
     auto soft = [&](f32x4_t (&st)[4], bf16x8_t (&pb)[2][NP]) __attribute__((always_inline)) {
-        float mx = -INFINITY;
+        float mx = max3(st[0][0], st[0][1], st[0][2]);
+        mx = max3(mx, st[0][3], st[1][0]);
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, st[kt][e]);
-        mx = rows_max(mx) * c;
+        for (int i = 5; i < 15; i += 2) mx = max3(mx, st[i / 4][i % 4], st[(i + 1) / 4][(i + 1) % 4]);
+        mx = rows_max(fmaxf(mx, st[3][3])) * c;
         const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
         if (__any(m_new > m)) {
             const float alpha = __builtin_amdgcn_exp2f(m - ref);
@@ -185,118 +209,157 @@ __global__ __launch_bounds__(256) void page_attention_kernel(PageAttnArgs a)
             cut_weights<NP>(p, pb[h2]);
         }
     };
-    // O^T += V^T P^T over the 32 staged rows, for one term of the values (VT: which) with the weights' terms that matter
-    auto values = [&](const bf16x8_t (&pb)[NP], int skip) __attribute__((always_inline)) {
+    // the 32 staged rows are this wave's alone, and its LDS accesses keep their order: only the compiler is held
+    auto hold = [&]() __attribute__((always_inline)) {
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+    // O^T += V^T P^T over them: one term of the values, with the weights' terms that matter (all but the last `skip`)
+    auto values = [&](const bf16x8_t (&pb)[NP], int skip) __attribute__((always_inline)) {
+        hold();
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
-            const bf16_t *src = s_v + (4 * gr + (n >> 2)) * RPV + dt * 16 + 4 * (n & 3);
+            unsigned char *src = s_v + (get ^ (uint32_t)(dt << 5));
             const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)src);
-            const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)(src + 16 * RPV));
+            const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)(src + 16 * 2 * D));
             const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
             for (int k = NP - 1; k >= 0; --k)
                 if (k + skip < NP) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[k], o[dt], 0, 0, 0);
         }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        hold();
     };
 
-    for (int ch = c0 + wave; ch < c1; ch += 4) {
+    // ---- rows of the store ----
+    int ch = c0 + wave;
+    for (; ch < min(sc, c1); ch += 4) {
         f32x4_t st[4];
         bf16x8_t pb[2][NP];
-        if (ch < sc) {
-            // ---- 64 rows of the store ----
-            const T *Kc = static_cast<const T *>(a.Kc) + (size_t)s * a.k_cap * D, *Vc = static_cast<const T *>(a.Vc) + (size_t)s * a.k_cap * D;
+        const T *Kc = static_cast<const T *>(a.Kc) + (size_t)s * a.k_cap * D, *Vc = static_cast<const T *>(a.Vc) + (size_t)s * a.k_cap * D;
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt) {
-                const int j0 = ch * 64 + kt * 16, j = min(j0 + n, kept - 1);
-                st[kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int kt = 0; kt < 4; ++kt) {
+            const int j0 = ch * 64 + kt * 16, j = min(j0 + n, kept - 1);
+            st[kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int kk = 0; kk < KS; ++kk) {
-                    bf16x8_t kf[NQ];
-                    Terms<T>::load(Kc + (size_t)j * D + gr * (D / 4) + kk * 8, kf);
+            for (int kk = 0; kk < KS; ++kk) {
+                bf16x8_t kf[NQ];
+                Terms<T>::load(Kc + (size_t)j * D + gr * (D / 4) + kk * 8, kf);
 #pragma unroll
-                    for (int x = NQ - 1; x >= 0; --x)
+                for (int x = NQ - 1; x >= 0; --x)
 #pragma unroll
-                        for (int y = NQ - 1 - x; y >= 0; --y) st[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x], qf[kk][y], st[kt], 0, 0, 0);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (j0 + 4 * gr + e >= kept) st[kt][e] = -INFINITY;
+                    for (int y = NQ - 1 - x; y >= 0; --y) st[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x], qf[kk][y], st[kt], 0, 0, 0);
             }
-            soft(st, pb);
 #pragma unroll
-            for (int h2 = 0; h2 < 2; ++h2)
+            for (int e = 0; e < 4; ++e)
+                if (j0 + 4 * gr + e >= kept) st[kt][e] = -INFINITY;
+        }
+        soft(st, pb);
 #pragma unroll
-                for (int x = NQ - 1; x >= 0; --x) {
+        for (int h2 = 0; h2 < 2; ++h2)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int j = ch * 64 + h2 * 32 + i * 16 + n;
+            for (int x = NQ - 1; x >= 0; --x) {
 #pragma unroll
-                        for (int kk = 0; kk < KS; ++kk) {
-                            bf16x8_t vf[NQ];
-                            Terms<T>::load(Vc + (size_t)min(j, kept - 1) * D + gr * (D / 4) + kk * 8, vf);
-                            if (j >= kept) vf[x] = __builtin_bit_cast(bf16x8_t, make_uint4(0u, 0u, 0u, 0u));
-                            *reinterpret_cast<bf16x8_t *>(s_v + (i * 16 + n) * RPV + gr * (D / 4) + kk * 8) = vf[x];
-                        }
+                for (int i = 0; i < 2; ++i) {
+                    const int j = ch * 64 + h2 * 32 + i * 16 + n;
+#pragma unroll
+                    for (int kk = 0; kk < KS; ++kk) {
+                        bf16x8_t vf[NQ];
+                        Terms<T>::load(Vc + (size_t)min(j, kept - 1) * D + gr * (D / 4) + kk * 8, vf);
+                        if (j >= kept) vf[x] = __builtin_bit_cast(bf16x8_t, make_uint4(0u, 0u, 0u, 0u));
+                        *reinterpret_cast<bf16x8_t *>(put[kk] + i * 16 * 2 * D) = vf[x];
                     }
-                    values(pb[h2], x);
                 }
-            continue;
-        }
-        // ---- 64 tokens of the pages ----
-        typedef typename Codes<D>::type codes_t;
-        const int t0 = base0 + (ch - sc) * 64;
-        codes_t kc[4], vc[4];
-        uint32_t sk[4], sv[4];
-        bool there[4];                            // this lane's token of the group is one that some query may see
+                values(pb[h2], x);
+            }
+    }
+
+    // ---- tokens of the pages ----
+    // Lane 4 j + i holds the page of group i of this wave's chunk j (of 16; -1: none), for the next 16 chunks as well.
+    const int32_t *table = a.table + (size_t)b * g.max_pages;
+    const int tok = base0 + (ch - sc) * 64;      // the first of this wave's chunks
+    const int mine = ch < c1 ? (c1 - ch + 3) >> 2 : 0;
+    auto lookup = [&](int j0) __attribute__((always_inline)) {
+        const int j = j0 + (lane >> 2);
+        if (j >= mine) return -1;
+        const int pi = (tok + j * 256 + (lane & 3) * 16) >> g.page_shift;
+        const int page = table[min(pi, g.max_pages - 1)];
+        return pi < g.max_pages && (uint32_t)page < (uint32_t)g.n_pages ? page : -1;
+    };
+    typedef typename Codes<D>::type codes_t;
+    const uint32_t at_codes = (uint32_t)lane_offset<D>(n, gr), at_scale = (uint32_t)(n * NB + gr * NB / 4) * 2;
+    codes_t kc[4], vc[4];
+    uint32_t sk[4], sv[4];                       // scale bytes: of the key, of the value in the byte above
+    const unsigned char *vbase[4];
+    int pv = lookup(0), pv_next = lookup(16);
+    auto fetch_keys = [&](int j) __attribute__((always_inline)) {
+        const int t0 = tok + j * 256;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int t = t0 + 16 * i, pi = t >> g.page_shift;
-            int page = pi < g.max_pages ? table[pi] : -1;
-            const bool ok = (uint32_t)page < (uint32_t)g.n_pages;
-            there[i] = ok && t + n >= first && t + n < len;
-            page = ok ? page : 0;
-            const unsigned char *p = pool + (size_t)page * g.Hkv * block + (size_t)((t & ((1 << g.page_shift) - 1)) >> 4) * group_bytes(D);
-            kc[i] = *reinterpret_cast<const codes_t *>(p + lane_offset<D>(n, gr));
-            vc[i] = *reinterpret_cast<const codes_t *>(p + 8 * D + lane_offset<D>(n, gr));
-            const uint32_t sc2 = *reinterpret_cast<const uint16_t *>(p + 16 * D + (n * NB + gr * NB / 4) * 2);
-            sk[i] = sc2 & 255u;
-            sv[i] = sc2 >> 8;
+            const int page = max(__builtin_amdgcn_readlane(pv, (j & 15) * 4 + i), 0);
+            const uint32_t in = (uint32_t)(t0 + 16 * i) & ((1u << g.page_shift) - 1u);
+            const unsigned char *p = pool + (size_t)(uint32_t)page * (uint32_t)g.Hkv * block + (size_t)(in >> 4) * group_bytes(D);
+            vbase[i] = p + 8 * D;
+            kc[i] = load_codes<STREAM, codes_t>(p, at_codes);
+            sk[i] = load_codes<STREAM, uint16_t>(p + 16 * D, at_scale);
         }
+    };
+    auto fetch_values = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (!there[i]) { kc[i] = codes_t{}; vc[i] = codes_t{}; sk[i] = sv[i] = 127u; }
+        for (int i = 0; i < 4; ++i) { vc[i] = load_codes<STREAM, codes_t>(vbase[i], at_codes); sv[i] = sk[i]; }
+    };
+    if (mine > 0) {
+        fetch_keys(0);
+        fetch_values();
+    }
+    for (int j = 0; j < mine; ++j) {
+        const int t0 = tok + j * 256;
+        const uint64_t none = __ballot(pv < 0);
+        const uint32_t gone = (uint32_t)(none >> ((j & 15) * 4)) & 15u;       // groups without a page
+        const bool full = gone == 0 && t0 >= first && t0 + 64 <= len && t0 + 63 <= lim_all;
+        // (what lies in no page, before `first` or behind the length may hold anything: its scores are replaced, its values are zeros)
+        if (!full) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if ((gone >> i & 1) || t0 + 16 * i + n < first || t0 + 16 * i + n >= len) { vc[i] = codes_t{}; sv[i] = 127u << 8; }
         }
+        f32x4_t st[4];
+        bf16x8_t pb[2][NP];
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
             st[kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int kk = 0; kk < KS; ++kk) {
-                const bf16x8_t kf = unpack8(kc[kt][kk], scale_of(sk[kt]));
+                const bf16x8_t kf = unpack8(kc[kt][kk], __uint_as_float(sk[kt] << 23));
 #pragma unroll
                 for (int y = NQ - 1; y >= 0; --y) st[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[kk][y], st[kt], 0, 0, 0);
             }
-            // tokens of this group that lie in a page, [first, len), as the lanes that loaded them saw it
-            const uint32_t held = (uint32_t)(__ballot(there[kt]) & 0xFFFFu);
+        }
+        if (j + 1 < mine) {
+            if ((j + 1) % 16 == 0) { pv = pv_next; pv_next = lookup(j + 17); }
+            fetch_keys(j + 1);
+        }
+        if (!full) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (!(held >> (4 * gr + e) & 1) || t0 + 16 * kt + 4 * gr + e > lim) st[kt][e] = -INFINITY;
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int t = t0 + 16 * kt + 4 * gr + e;
+                    if ((gone >> kt & 1) || t < first || t > lim) st[kt][e] = -INFINITY;
+                }
         }
         soft(st, pb);
+        if (__any(max(max(sv[0], sv[1]), max(sv[2], sv[3])) >= kNanScale << 8)) {       // (rare)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint64_t bad = __ballot(sv[i] == kNanScale);
-            while (bad) {                        // (rare)
-                const int x = __builtin_ctzll(bad);
-                bad &= bad - 1;
-                if (t0 + 16 * i + (x & 15) <= lim) nan_blocks |= 1u << ((x >> 4) * NB / 4);
+            for (int i = 0; i < 4; ++i) {
+                uint64_t bad = __ballot(sv[i] >= kNanScale << 8);
+                while (bad) {
+                    const int x = __builtin_ctzll(bad);
+                    bad &= bad - 1;
+                    if (t0 + 16 * i + (x & 15) <= lim) nan_blocks |= 1u << ((x >> 4) * NB / 4);
+                }
+                if (sv[i] >= kNanScale << 8) { vc[i] = codes_t{}; sv[i] = 127u << 8; }
             }
-            if (sv[i] == kNanScale) { vc[i] = codes_t{}; sv[i] = 127u; }
         }
 #pragma unroll
         for (int h2 = 0; h2 < 2; ++h2) {
@@ -304,7 +367,8 @@ __global__ __launch_bounds__(256) void page_attention_kernel(PageAttnArgs a)
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int kk = 0; kk < KS; ++kk)
-                    *reinterpret_cast<bf16x8_t *>(s_v + (i * 16 + n) * RPV + gr * (D / 4) + kk * 8) = unpack8(vc[2 * h2 + i][kk], scale_of(sv[2 * h2 + i]));
+                    *reinterpret_cast<bf16x8_t *>(put[kk] + i * 16 * 2 * D) = unpack8(vc[2 * h2 + i][kk], __uint_as_float(sv[2 * h2 + i] << 15));
+            if (h2 == 1 && j + 1 < mine) fetch_values();
             values(pb[h2], 0);
         }
     }
@@ -322,8 +386,8 @@ __global__ __launch_bounds__(256) void page_attention_kernel(PageAttnArgs a)
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t *>(s_o + (wave * 16 + n) * OP + dt * 16 + 4 * gr) = o[dt];
     __syncthreads();
-    constexpr int EPT = D / 16;                  // elements of a thread: 16 threads per query
-    const int oq = tid >> 4, oe = (tid & 15) * EPT, orr = qt * 16 + oq;
+    constexpr int EPT = D / 16;                  // elements of a thread: 16 threads per query, their elements 16 apart
+    const int oq = tid >> 4, oe = tid & 15, orr = qt * 16 + oq;
     float M = s_m[0][oq];
 #pragma unroll
     for (int w = 1; w < 4; ++w) M = fmaxf(M, s_m[w][oq]);
@@ -334,22 +398,26 @@ __global__ __launch_bounds__(256) void page_attention_kernel(PageAttnArgs a)
         const float f = __builtin_amdgcn_exp2f(s_m[w][oq] - Mr);
         L += s_l[w][oq] * f;
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) acc[e] += s_o[(w * 16 + oq) * OP + oe + e] * f;
+        for (int e = 0; e < EPT; ++e) acc[e] += s_o[(w * 16 + oq) * OP + oe + 16 * e] * f;
     }
-    const int ogq = orr / a.Tq, otq = orr - ogq * a.Tq;
-    T *O = static_cast<T *>(a.O) + ((((size_t)lb * g.Hkv + h) * a.G + ogq) * a.Tq + otq) * D + oe;
+    // where query q of the unit's output begins
+    auto out_of = [&](int q) __attribute__((always_inline)) {
+        const int x = qt * 16 + q, xg = x / a.Tq;
+        return static_cast<T *>(a.O) + ((((size_t)lb * g.Hkv + h) * a.G + xg) * a.Tq + (x - xg * a.Tq)) * D;
+    };
     if (active == 1) {
         if (orr < R) {
-            const float inv = L == 0.f ? 0.f : 1.0f / L;         // (no rows: 0; a NaN stays one)
+            const float inv = 1.0f / L;                          // (no rows: 0 below; a NaN stays one)
+            T *O = out_of(oq);
 #pragma unroll
-            for (int e = 0; e < EPT; ++e) Storage<T>::store(O + e, L == 0.f ? 0.f : acc[e] * inv);
+            for (int e = 0; e < EPT; ++e) Storage<T>::store(O + oe + 16 * e, L == 0.f ? 0.f : acc[e] * inv);
         }
         return;
     }
-    float *part = a.part + (((size_t)unit * a.nsplit + split) * 16 + oq) * (D + 2);
     if (orr < R) {
+        float *part = a.part + (((size_t)unit * a.nsplit + split) * 16 + oq) * (D + 2);
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) store_device(part + oe + e, acc[e]);
+        for (int e = 0; e < EPT; ++e) store_device(part + oe + 16 * e, acc[e]);
         if (oe == 0) { store_device(part + D, M); store_device(part + D + 1, L); }
     }
     // ---- the workgroups meet: as in decode attention ----
@@ -360,37 +428,76 @@ __global__ __launch_bounds__(256) void page_attention_kernel(PageAttnArgs a)
     __syncthreads();
     if (!s_last) return;
     if (tid == 0) __hip_atomic_store(a.tickets + unit, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (orr >= R) return;
-    part = a.part + ((size_t)unit * a.nsplit * 16 + oq) * (D + 2);
-    M = -INFINITY;
-    for (int x = 0; x < active; ++x) M = fmaxf(M, load_device(part + (size_t)x * 16 * (D + 2) + D));
-    const float ref = M == -INFINITY ? 0.f : M;
+    // Few queries leave most of the 16 rows of threads idle: those take partials side by side (row q + Q k: partials k, k + 16 / Q, ...
+    // of query q), which are added up in LDS in that order.
+    const int live = min(16, R - qt * 16);
+    int lq = 0;
+    while (1 << lq < live) ++lq;
+    const int Q = 1 << lq, q = oq & (Q - 1), k0 = oq >> lq, kn = 16 >> lq;
     L = 0.f;
+    M = -INFINITY;
 #pragma unroll
     for (int e = 0; e < EPT; ++e) acc[e] = 0.f;
-    for (int x = 0; x < active; ++x) {
-        const float *pp = part + (size_t)x * 16 * (D + 2);
-        const float f = __builtin_amdgcn_exp2f(load_device(pp + D) - ref);
-        L += load_device(pp + D + 1) * f;
+    if (q < live) {
+        const float *part = a.part + ((size_t)unit * a.nsplit * 16 + q) * (D + 2);
+#pragma unroll 2
+        for (int x = k0; x < active; x += kn) {
+            const float *pp = part + (size_t)x * 16 * (D + 2);
+            const float px = load_device(pp + D), pl = load_device(pp + D + 1);
+            float v[EPT];
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) acc[e] += load_device(pp + oe + e) * f;
+            for (int e = 0; e < EPT; ++e) v[e] = load_device(pp + oe + 16 * e);
+            const float Mn = fmaxf(M, px), ref = Mn == -INFINITY ? 0.f : Mn, f0 = __builtin_amdgcn_exp2f(M - ref), f1 = __builtin_amdgcn_exp2f(px - ref);
+            L = L * f0 + pl * f1;
+#pragma unroll
+            for (int e = 0; e < EPT; ++e) acc[e] = acc[e] * f0 + v[e] * f1;
+            M = Mn;
+        }
     }
-    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    if (kn > 1) {
+        // (reads of s_o and s_m by the first merge lie behind the barriers of the ticket)
+        float *mm = &s_m[0][0], *ll = &s_l[0][0];
+        if (oe == 0) { mm[oq] = M; ll[oq] = L; }
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) Storage<T>::store(O + e, L == 0.f ? 0.f : acc[e] * inv);
+        for (int e = 0; e < EPT; ++e) s_o[oq * OP + oe + 16 * e] = acc[e];
+        __syncthreads();
+        if (k0 != 0) return;
+        M = -INFINITY;
+        for (int k = 0; k < kn; ++k) M = fmaxf(M, mm[q + Q * k]);
+        const float ref = M == -INFINITY ? 0.f : M;
+        L = 0.f;
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) acc[e] = 0.f;
+        for (int k = 0; k < kn; ++k) {
+            const float f = __builtin_amdgcn_exp2f(mm[q + Q * k] - ref);
+            L += ll[q + Q * k] * f;
+#pragma unroll
+            for (int e = 0; e < EPT; ++e) acc[e] += s_o[(q + Q * k) * OP + oe + 16 * e] * f;
+        }
+    }
+    if (q >= live) return;
+    T *O = out_of(q);
+    const float inv = 1.0f / L;
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) Storage<T>::store(O + oe + 16 * e, L == 0.f ? 0.f : acc[e] * inv);
 #endif
+}
+
+template <typename T, int D> static void launch_page_attention_as(const PageAttnArgs &a, dim3 grid, hipStream_t st)
+{
+    if (a.stream) hipLaunchKernelGGL((page_attention_kernel<T, D, true>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((page_attention_kernel<T, D, false>), grid, dim3(256), 0, st, a);
 }
 
 hipError_t launch_page_attention(const PageAttnArgs &a, int dtype, hipStream_t st)
 {
-    const int64_t blocks = (int64_t)a.g.L * a.g.B * a.g.Hkv * a.qtiles * a.nsplit;
-    const dim3 grid((unsigned)blocks), block(256);
+    const dim3 grid((unsigned)((int64_t)a.g.L * a.g.B * a.g.Hkv * a.qtiles * a.nsplit));
     if (dtype == KVEV_F32) {
-        if (a.g.d == 128) hipLaunchKernelGGL((page_attention_kernel<float, 128>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((page_attention_kernel<float, 64>), grid, block, 0, st, a);
+        if (a.g.d == 128) launch_page_attention_as<float, 128>(a, grid, st);
+        else launch_page_attention_as<float, 64>(a, grid, st);
     } else {
-        if (a.g.d == 128) hipLaunchKernelGGL((page_attention_kernel<bf16_t, 128>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((page_attention_kernel<bf16_t, 64>), grid, block, 0, st, a);
+        if (a.g.d == 128) launch_page_attention_as<bf16_t, 128>(a, grid, st);
+        else launch_page_attention_as<bf16_t, 64>(a, grid, st);
     }
     return hipGetLastError();
 }

@@ -56,6 +56,7 @@ struct PageAttnArgs {
     int min_chunks;               // fewest chunks of 64 rows worth a workgroup
     float *part;                  // [unit's queries][nsplit][d + 2]
     int32_t *tickets;             // one per unit, zero between calls
+    int stream;                   // 1: more than the memory-side cache holds is read: loads carry the non-temporal hint
     float scale_log2e;
 };
 
