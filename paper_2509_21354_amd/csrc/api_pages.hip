@@ -40,23 +40,43 @@ static size_t elem(const kvev_shape *sh) { return sh->dtype == KVEV_F32 ? 4 : 2;
 static size_t pool_bytes(const PageGeom &g) { return (size_t)g.L * g.n_pages * page_bytes(g); }
 
 // ---- attention over pages: planning ----
-// A unit is 16 queries of a key-value head; its rows are shared by up to nsplit workgroups, and a row of the batch takes as many of
-// them as its own length pays for (decided on the device: the lengths are there).  shape->T, or the capacity if it is 0, says for
-// which length nsplit is made; results do not depend on it beyond the order of sums.
-constexpr int kPageChunk = 64, kPageMaxSplit = 64, kPageMinChunks = 4;
-struct PageAttnPlan { int qtiles, nsplit; int64_t units; size_t ticket_bytes, ws_bytes; };
+// A unit is 16 queries of a key-value head; its rows, in chunks of 64 (one for each of a workgroup's 4 waves in turn), are cut into
+// runs of `run` chunks, a workgroup each.  A batch row takes as many of a unit's nsplit workgroups as its own length pays for
+// (decided on the device, where the lengths are).  shape->T, or the capacity if it is 0, says for which length the launch is made;
+// results depend on it in the order of sums only.
+//   * Runs of 4 chunks and more, so that the units take one workgroup per compute unit: 32 units x 4091 tokens 11.4 us, with two or
+//     four per compute unit 13.0; 8 units x 16000 tokens 14.7 and 20 us.
+//   * Up to 8 chunks one run: 32 x 300 tokens 7.6 us, in two runs 8.5; 8 units x 500 tokens 7.5 and 7.8 us.  (32 x 1000: 8.8 us in
+//     runs of 4, 10.4 in runs of 8.)
+//   * Where such a run would be longer than 16 chunks, runs for four workgroups per compute unit, of 16 chunks at least: they hide
+//     each other's ends, and long rows of a ragged batch are spread (32 x 16000 tokens 19.9 us, one workgroup per compute unit 22.0;
+//     512 units of 64 ragged rows up to 8192 tokens 63 us, unsplit 72; 128 units of 16 ragged rows up to 12000 29 and 47 us).
+constexpr int kPageChunk = 64, kPageMaxSplit = 64;
+struct PageAttnPlan { int qtiles, nsplit, run; int64_t units; size_t ticket_bytes, ws_bytes; };
 static PageAttnPlan plan_page_attn(const kvev_shape *sh, const PageGeom &g, int Tq, int64_t tokens)
 {
     PageAttnPlan p;
     const int64_t R = (int64_t)(sh->H / g.Hkv) * Tq;
     p.qtiles = (int)((R + 15) / 16);
     p.units = (int64_t)g.L * g.B * g.Hkv * p.qtiles;
-    const int64_t chunks = (tokens + kPageChunk - 1) / kPageChunk, target = 4 * (int64_t)device_compute_units();
-    const int64_t want = std::min((target + p.units - 1) / p.units, (chunks + kPageMinChunks - 1) / kPageMinChunks);
-    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(want, kPageMaxSplit));
+    const int64_t chunks = (tokens + kPageChunk - 1) / kPageChunk, cus = device_compute_units();
+    int64_t run = std::max<int64_t>((chunks * p.units + cus - 1) / cus, chunks <= 8 ? 8 : 4);
+    if (run > 16) run = std::max<int64_t>(16, (chunks * p.units + 4 * cus - 1) / (4 * cus));
+    run = std::min(std::max(run, (chunks + kPageMaxSplit - 1) / kPageMaxSplit), std::max<int64_t>(chunks, 1));
+    p.run = (int)run;
+    p.nsplit = (int)std::max<int64_t>(1, (chunks + run - 1) / run);
     p.ticket_bytes = ((size_t)p.units * sizeof(int32_t) + 255) / 256 * 256;
     p.ws_bytes = p.nsplit > 1 ? p.ticket_bytes + (size_t)p.units * p.nsplit * 16 * (g.d + 2) * sizeof(float) : 0;
     return p;
+}
+// Scratch that is enough for every length of row: by either border of `run`, no more than 4 compute units' worth of runs to a unit
+// (rounded up), and none shorter than 4 chunks.
+static size_t page_attn_scratch(const kvev_shape *sh, const PageGeom &g, int Tq)
+{
+    const int64_t cap = (int64_t)g.max_pages << g.page_shift;
+    const PageAttnPlan p = plan_page_attn(sh, g, Tq, cap);
+    const int64_t most = std::min<int64_t>({kPageMaxSplit, (4 * (int64_t)device_compute_units() + p.units - 1) / p.units, (cap / kPageChunk + 4) / 4});
+    return most > 1 ? p.ticket_bytes + (size_t)p.units * most * 16 * (g.d + 2) * sizeof(float) : 0;
 }
 static int64_t plan_tokens(const kvev_shape *sh, const PageGeom &g)
 {
@@ -100,7 +120,7 @@ size_t kvev_page_workspace_bytes(int op, const kvev_shape *sh, const kvev_pages 
     if (check_pages(sh, pg, &g) != KVEV_OK || n < 0) return 0;
     switch (op) {
     case KVEV_OP_PAGE_ATTENTION:
-        return n == 0 ? 0 : plan_page_attn(sh, g, n, (int64_t)g.max_pages << g.page_shift).ws_bytes;
+        return n == 0 ? 0 : page_attn_scratch(sh, g, n);
     case KVEV_OP_PAGES_RESERVE:
         return reserve_words(g) * 4;
     case KVEV_OP_PAGES_COMPACT:
@@ -189,7 +209,7 @@ int kvev_page_attention(const kvev_shape *sh, const kvev_pages *pg, const void *
     if (p.ws_bytes > 0 && (!whole16(ws) || ws_bytes < p.ws_bytes)) return KVEV_ERR_WORKSPACE;
     a.Q = Q; a.O = O; a.pool = static_cast<const unsigned char *>(pool); a.table = table; a.length = length; a.first = first; a.q_start = q_start;
     if (k_cap > 0) { a.Kc = Kc; a.Vc = Vc; a.count = count; a.k_cap = k_cap; }
-    a.G = sh->H / a.g.Hkv; a.Tq = Tq; a.nsplit = p.nsplit; a.qtiles = p.qtiles; a.min_chunks = kPageMinChunks;
+    a.G = sh->H / a.g.Hkv; a.Tq = Tq; a.nsplit = p.nsplit; a.qtiles = p.qtiles; a.run = p.run;
     if (p.nsplit > 1) {
         a.tickets = static_cast<int32_t *>(ws);
         a.part = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + p.ticket_bytes);

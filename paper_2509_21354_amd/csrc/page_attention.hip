@@ -123,24 +123,36 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
     const PageGeom &g = a.g;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, gr = lane >> 4;
-    uint32_t blk = blockIdx.x;
-    const int split = (int)(blk % (uint32_t)a.nsplit); blk /= (uint32_t)a.nsplit;
-    const int unit = (int)blk;
+    // (workgroups go round-robin over the 8 XCDs: with the runs of a unit side by side, those that short rows of the batch do not
+    // take would leave some XCDs idle)
+    const int units = (int)(gridDim.x / (uint32_t)a.nsplit), split = (int)(blockIdx.x / (uint32_t)units), unit = (int)(blockIdx.x % (uint32_t)units);
     const int qt = unit % a.qtiles, s = unit / a.qtiles, h = s % g.Hkv, lb = s / g.Hkv, b = lb % g.B, l = lb / g.B;
     const int R = a.G * a.Tq, cap = g.max_pages << g.page_shift;
+
+    // this lane's query
+    const int r = qt * 16 + n, rc = min(r, R - 1), gq = rc / a.Tq, tq = rc - gq * a.Tq;
+    const size_t orow = (((size_t)lb * g.Hkv + h) * a.G + gq) * a.Tq + tq;
+    bf16x8_t qf[KS][NQ];
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) Terms<T>::load(static_cast<const T *>(a.Q) + orow * D + gr * (D / 4) + kk * 8, qf[kk]);
+
+    // Lane 4 j + i holds the table's entry for group i of this wave's chunk j (of 16): asked for before the length is there, as if
+    // the rows were the pages' from the beginning on and the run as long as planned, which they are most of the time.
+    const int32_t *table = a.table + (size_t)b * g.max_pages;
+    const uint32_t ahead = (uint32_t)((lane >> 2) * 256 + (lane & 3) * 16);
+    auto entry = [&](uint32_t t) __attribute__((always_inline)) { return table[min((t + ahead) >> g.page_shift, (uint32_t)g.max_pages - 1u)]; };
+    const uint32_t guess = ((uint32_t)split * (uint32_t)a.run + (uint32_t)wave) * 64u;
+    int pv = entry(guess);
 
     // the rows of this unit in chunks of 64: the store's, then the pages' from the chunk of `first` on
     const int len = min(max(a.length[b], 0), cap), first = a.first ? min(max(a.first[b], 0), len) : 0;
     const int kept = a.count ? min(max(a.count[s], 0), a.k_cap) : 0;
     const int sc = (kept + 63) >> 6, base0 = first & ~63, pc = (len - base0 + 63) >> 6, chunks = sc + pc;
-    const int per = max(a.min_chunks, (chunks + a.nsplit - 1) / a.nsplit), active = max(1, (chunks + per - 1) / per);
+    const int per = max(a.run, (chunks + a.nsplit - 1) / a.nsplit), active = max(1, (chunks + per - 1) / per);
     if (split >= active) return;
     const int c0 = split * per, c1 = min(chunks, c0 + per);
 
-    // this lane's query, and the last token that it sees
-    const int r = qt * 16 + n, rc = min(r, R - 1), gq = rc / a.Tq, tq = rc - gq * a.Tq;
-    const size_t orow = (((size_t)lb * g.Hkv + h) * a.G + gq) * a.Tq + tq;
-    int lim = len - 1, lim_all = len - 1;        // ... and the last one that all of the unit's queries see
+    int lim = len - 1, lim_all = len - 1;        // the last token that this lane's query sees, and that all of the unit's see
     if (a.q_start) {
         const int64_t at = a.q_start[b];
         lim = (int)min<int64_t>(lim, at + tq);
@@ -148,9 +160,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
         const int t0 = qt * 16 / a.Tq == min(qt * 16 + 15, R - 1) / a.Tq ? qt * 16 % a.Tq : 0;
         lim_all = (int)min<int64_t>(lim_all, at + t0);
     }
-    bf16x8_t qf[KS][NQ];
-#pragma unroll
-    for (int kk = 0; kk < KS; ++kk) Terms<T>::load(static_cast<const T *>(a.Q) + orow * D + gr * (D / 4) + kk * 8, qf[kk]);
 
     float m = -INFINITY, lsum = 0.f;             // scaled running maximum and this lane's part of the sum, of query n
     f32x4_t o[DT];
@@ -275,23 +284,21 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
     }
 
     // ---- tokens of the pages ----
-    // Lane 4 j + i holds the page of group i of this wave's chunk j (of 16; -1: none), for the next 16 chunks as well.
-    const int32_t *table = a.table + (size_t)b * g.max_pages;
     const int tok = base0 + (ch - sc) * 64;      // the first of this wave's chunks
     const int mine = ch < c1 ? (c1 - ch + 3) >> 2 : 0;
-    auto lookup = [&](int j0) __attribute__((always_inline)) {
-        const int j = j0 + (lane >> 2);
-        if (j >= mine) return -1;
-        const int pi = (tok + j * 256 + (lane & 3) * 16) >> g.page_shift;
-        const int page = table[min(pi, g.max_pages - 1)];
-        return pi < g.max_pages && (uint32_t)page < (uint32_t)g.n_pages ? page : -1;
+    if ((uint32_t)tok != guess) pv = entry((uint32_t)tok);
+    // the pages of chunks j0 .. j0 + 15 from their entries; -1: none
+    auto checked = [&](int e, int j0) __attribute__((always_inline)) {
+        const uint32_t pi = ((uint32_t)tok + (uint32_t)j0 * 256u + ahead) >> g.page_shift;
+        return j0 + (lane >> 2) < mine && pi < (uint32_t)g.max_pages && (uint32_t)e < (uint32_t)g.n_pages ? e : -1;
     };
     typedef typename Codes<D>::type codes_t;
     const uint32_t at_codes = (uint32_t)lane_offset<D>(n, gr), at_scale = (uint32_t)(n * NB + gr * NB / 4) * 2;
     codes_t kc[4], vc[4];
     uint32_t sk[4], sv[4];                       // scale bytes: of the key, of the value in the byte above
     const unsigned char *vbase[4];
-    int pv = lookup(0), pv_next = lookup(16);
+    pv = checked(pv, 0);
+    int pv_next = entry((uint32_t)tok + 16u * 256u);
     auto fetch_keys = [&](int j) __attribute__((always_inline)) {
         const int t0 = tok + j * 256;
 #pragma unroll
@@ -336,7 +343,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
             }
         }
         if (j + 1 < mine) {
-            if ((j + 1) % 16 == 0) { pv = pv_next; pv_next = lookup(j + 17); }
+            if ((j + 1) % 16 == 0) {
+                pv = checked(pv_next, j + 1);
+                pv_next = entry((uint32_t)tok + (uint32_t)(j + 17) * 256u);
+            }
             fetch_keys(j + 1);
         }
         if (!full) {

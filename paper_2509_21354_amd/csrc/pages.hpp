@@ -53,7 +53,7 @@ struct PageAttnArgs {
     int G, Tq;
     int nsplit;                   // most workgroups that share a unit's rows
     int qtiles;                   // units per key-value head: its queries in tiles
-    int min_chunks;               // fewest chunks of 64 rows worth a workgroup
+    int run;                      // chunks of 64 rows for a workgroup (more where rows are longer than planned for)
     float *part;                  // [unit's queries][nsplit][d + 2]
     int32_t *tickets;             // one per unit, zero between calls
     int stream;                   // 1: more than the memory-side cache holds is read: loads carry the non-temporal hint
