@@ -351,8 +351,11 @@ int kvev_page_read(const kvev_shape *shape, const kvev_pages *pages, const void 
  * a padded batch, queries from n_new[b] on get some finite output that means nothing.)  Tokens without a
  * page are left out.  A query that sees no row gives zeros.
  * Scores, softmax and sums are fp32, O is rounded once.  fp32: operands enter the matrix
- * cores as three bf16 terms; bf16: the softmax weights as two, 16 significant bits.  shape->T (0: the capacity) says for what length of row the launch is made; any
- * length is right, and results depend on it in the order of sums only.
+ * cores as three bf16 terms; bf16: the softmax weights as two, 16 significant bits, or as one
+ * rounded to bf16 in frames (48 queries or more to a key-value head, and enough rows to pay for the
+ * form), whose normaliser sums them unrounded as in kvev_gated_attention.  shape->T (0: the
+ * capacity) says for what length of row the launch is made; any length is right, and results
+ * depend on it in the order of sums and the choice of the form only.
  * Workspace: kvev_page_workspace_bytes(KVEV_OP_PAGE_ATTENTION, shape, pages, Tq), enough for
  * every T; zero-filled before its first use, tickets as in kvev_gated_attention.  O must not overlap Q. */
 int kvev_page_attention(const kvev_shape *shape, const kvev_pages *pages, const void *Q, int Tq, const void *pool,

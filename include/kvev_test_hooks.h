@@ -66,6 +66,16 @@ int kvev_debug_decode_queries(const kvev_shape *shape, int Tq, int k_cap, int *q
  * none (always KVEV_OK). */
 int kvev_debug_attn_stream_bytes(size_t bytes);
 
+/* kvev_page_attention takes calls of bf16 storage with 48 queries or more to a
+ * key-value head as frames when they come to `work` units of 16 queries x tokens
+ * (0 restores the default).  Lowering it to 1 lets small shapes walk the frame
+ * kernels.  Errors: INVALID_ARG for a negative value. */
+int kvev_debug_page_frame_work(int64_t work);
+
+/* How a kvev_page_attention call would run: queries of a unit (16; a frame's 128
+ * or 256) and the most workgroups that share a unit's rows.  Errors: INVALID_ARG. */
+int kvev_debug_page_form(const kvev_shape *shape, const kvev_pages *pages, int Tq, int *queries, int *runs);
+
 /* Calibration of the memory system for the benchmark's roofline notes (bench.py
  * --calibrate-stream): a plain streaming kernel, one workgroup per tile, reads
  * src_bytes of device memory in tiles of tile_bytes (a multiple of 4096 that

@@ -132,6 +132,7 @@ static AttnPlan plan_attn(const kvev_shape *sh, int Tq, int n_rows)
 
 // single-query launches that read more than this take their rows with the non-temporal hint
 static std::atomic<size_t> g_stream_bytes{kCacheBytes};
+size_t attn_stream_bytes() { return g_stream_bytes.load(std::memory_order_relaxed); }
 
 // a frame of queries per key-value sequence (all heads of a group count) goes to the matrix cores
 static bool attn_takes_mq(const kvev_shape *sh, int Tq)

@@ -4,7 +4,9 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 
+#include "../../include/kvev_test_hooks.h"
 #include "api.hpp"
 #include "kernels.hpp"
 #include "pages.hpp"
@@ -51,32 +53,46 @@ static size_t pool_bytes(const PageGeom &g) { return (size_t)g.L * g.n_pages * p
 //   * Where such a run would be longer than 16 chunks, runs for four workgroups per compute unit, of 16 chunks at least: they hide
 //     each other's ends, and long rows of a ragged batch are spread (32 x 16000 tokens 19.9 us, one workgroup per compute unit 22.0;
 //     512 units of 64 ragged rows up to 8192 tokens 63 us, unsplit 72; 128 units of 16 ragged rows up to 12000 29 and 47 us).
-constexpr int kPageChunk = 64, kPageMaxSplit = 64;
-struct PageAttnPlan { int qtiles, nsplit, run; int64_t units; size_t ticket_bytes, ws_bytes; };
-static PageAttnPlan plan_page_attn(const kvev_shape *sh, const PageGeom &g, int Tq, int64_t tokens)
+// Frames (page_frame.hip; bf16): units of 128 or 256 queries, two workgroups or one per compute unit, runs of 4 chunks and more so
+// that one round of workgroups fills the chip.  They take calls with 48 queries or more to a key-value head and enough work
+// (units of 16 queries x tokens; 4 query heads to a key-value head, units of 16 and frame, us): 128 heads x 64 queries x 4000
+// tokens 54.2 and 52.6; 128 x 128 x 600 24.2 and 26.0; 128 x 256 x 600 34.7 and 33.9; 512 x 64 x 600 40.8 and 32.6; 8 x 1024 x
+// 4000 47.8 and 41.8; but 8 x 1024 x 600 12.9 and 23.5, 8 x 256 x 4000 19.9 and 34.4, and 512 x 32 x 4000 106 and 124.
+constexpr int kPageChunk = 64, kPageMaxSplit = 64, kFrameQueries = 48;
+constexpr int64_t kFrameWork = 1200000;
+static std::atomic<int64_t> g_frame_work{kFrameWork};      // (kvev_debug_page_frame_work lowers it)
+struct PageAttnPlan { int queries, qtiles, nsplit, run; int64_t units; size_t ticket_bytes, ws_bytes, ws_any; };
+static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int Tq, int64_t tokens, bool frame)
 {
     PageAttnPlan p;
-    const int64_t R = (int64_t)(sh->H / g.Hkv) * Tq;
-    p.qtiles = (int)((R + 15) / 16);
+    const int64_t R = (int64_t)(sh->H / g.Hkv) * Tq, cus = device_compute_units(), cap = (int64_t)g.max_pages << g.page_shift;
+    p.queries = !frame ? 16 : R <= 128 ? 128 : 256;
+    p.qtiles = (int)((R + p.queries - 1) / p.queries);
     p.units = (int64_t)g.L * g.B * g.Hkv * p.qtiles;
-    const int64_t chunks = (tokens + kPageChunk - 1) / kPageChunk, cus = device_compute_units();
-    int64_t run = std::max<int64_t>((chunks * p.units + cus - 1) / cus, chunks <= 8 ? 8 : 4);
-    if (run > 16) run = std::max<int64_t>(16, (chunks * p.units + 4 * cus - 1) / (4 * cus));
+    const int64_t chunks = (tokens + kPageChunk - 1) / kPageChunk, slots = p.queries == 128 ? 2 * cus : cus;
+    int64_t run = std::max<int64_t>((chunks * p.units + slots - 1) / slots, !frame && chunks <= 8 ? 8 : 4);
+    if (!frame && run > 16) run = std::max<int64_t>(16, (chunks * p.units + 4 * slots - 1) / (4 * slots));
     run = std::min(std::max(run, (chunks + kPageMaxSplit - 1) / kPageMaxSplit), std::max<int64_t>(chunks, 1));
     p.run = (int)run;
     p.nsplit = (int)std::max<int64_t>(1, (chunks + run - 1) / run);
+    // tickets, then the partials of every run: 16 queries' outputs, maxima and sums, or the waves' of a frame as they hold them
     p.ticket_bytes = ((size_t)p.units * sizeof(int32_t) + 255) / 256 * 256;
-    p.ws_bytes = p.nsplit > 1 ? p.ticket_bytes + (size_t)p.units * p.nsplit * 16 * (g.d + 2) * sizeof(float) : 0;
+    const size_t partial = (!frame ? (size_t)16 * (g.d + 2) : (size_t)p.queries * (g.d + 4)) * sizeof(float);
+    auto scratch = [&](int64_t n) { return n > 1 ? p.ticket_bytes + (size_t)p.units * n * partial : (size_t)0; };
+    p.ws_bytes = scratch(p.nsplit);
+    // enough for every length of row: a unit takes no more than its share of the workgroups wanted (rounded up), and no run is
+    // shorter than 4 chunks
+    const int64_t wanted = frame ? slots : 4 * slots;
+    p.ws_any = scratch(std::min<int64_t>({kPageMaxSplit, (wanted + p.units - 1) / p.units, (cap / kPageChunk + 4) / 4}));
     return p;
 }
-// Scratch that is enough for every length of row: by either border of `run`, no more than 4 compute units' worth of runs to a unit
-// (rounded up), and none shorter than 4 chunks.
-static size_t page_attn_scratch(const kvev_shape *sh, const PageGeom &g, int Tq)
+static PageAttnPlan plan_page_attn(const kvev_shape *sh, const PageGeom &g, int Tq, int64_t tokens)
 {
-    const int64_t cap = (int64_t)g.max_pages << g.page_shift;
-    const PageAttnPlan p = plan_page_attn(sh, g, Tq, cap);
-    const int64_t most = std::min<int64_t>({kPageMaxSplit, (4 * (int64_t)device_compute_units() + p.units - 1) / p.units, (cap / kPageChunk + 4) / 4});
-    return most > 1 ? p.ticket_bytes + (size_t)p.units * most * 16 * (g.d + 2) * sizeof(float) : 0;
+    PageAttnPlan p = plan_page_form(sh, g, Tq, tokens, false);
+    if (sh->dtype != KVEV_BF16 || (int64_t)(sh->H / g.Hkv) * Tq < kFrameQueries) return p;
+    PageAttnPlan f = plan_page_form(sh, g, Tq, tokens, true);
+    f.ws_any = p.ws_any = std::max(p.ws_any, f.ws_any);      // (the form depends on the length as well)
+    return p.units * tokens >= g_frame_work.load() ? f : p;
 }
 static int64_t plan_tokens(const kvev_shape *sh, const PageGeom &g)
 {
@@ -108,6 +124,23 @@ using namespace kvev;
 
 extern "C" {
 
+int kvev_debug_page_frame_work(int64_t work)
+{
+    if (work < 0) return KVEV_ERR_INVALID_ARG;
+    g_frame_work = work == 0 ? kFrameWork : work;
+    return KVEV_OK;
+}
+
+int kvev_debug_page_form(const kvev_shape *sh, const kvev_pages *pg, int Tq, int *queries, int *runs)
+{
+    PageGeom g;
+    if (check_pages(sh, pg, &g) != KVEV_OK || Tq < 1 || !queries || !runs) return KVEV_ERR_INVALID_ARG;
+    const PageAttnPlan p = plan_page_attn(sh, g, Tq, plan_tokens(sh, g));
+    *queries = p.queries;
+    *runs = p.nsplit;
+    return KVEV_OK;
+}
+
 size_t kvev_page_pool_bytes(const kvev_shape *sh, const kvev_pages *pg)
 {
     PageGeom g;
@@ -120,7 +153,7 @@ size_t kvev_page_workspace_bytes(int op, const kvev_shape *sh, const kvev_pages 
     if (check_pages(sh, pg, &g) != KVEV_OK || n < 0) return 0;
     switch (op) {
     case KVEV_OP_PAGE_ATTENTION:
-        return n == 0 ? 0 : page_attn_scratch(sh, g, n);
+        return n == 0 ? 0 : plan_page_attn(sh, g, n, plan_tokens(sh, g)).ws_any;
     case KVEV_OP_PAGES_RESERVE:
         return reserve_words(g) * 4;
     case KVEV_OP_PAGES_COMPACT:
@@ -214,9 +247,10 @@ int kvev_page_attention(const kvev_shape *sh, const kvev_pages *pg, const void *
         a.tickets = static_cast<int32_t *>(ws);
         a.part = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + p.ticket_bytes);
     }
-    a.stream = (size_t)sh->L * sh->B * a.g.Hkv * (size_t)plan_tokens(sh, a.g) * 17 * sh->d / 16 > kCacheBytes;
+    a.stream = (size_t)sh->L * sh->B * a.g.Hkv * (size_t)plan_tokens(sh, a.g) * 17 * sh->d / 16 > attn_stream_bytes();
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)sh->d));
-    const hipError_t e = launch_page_attention(a, sh->dtype, static_cast<hipStream_t>(stream));
+    const hipError_t e = p.queries == 16 ? launch_page_attention(a, sh->dtype, static_cast<hipStream_t>(stream))
+                                         : launch_page_frame(a, p.queries, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? KVEV_OK : hip_fail(e);
 }
 

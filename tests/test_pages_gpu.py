@@ -210,7 +210,7 @@ def check_attention(c, Q, O, lengths, first=None, q_start=None, store=None, head
             vis = np.concatenate((np.ones((G, Tq, m), bool), vis), 2)
         want, E, S = ref.attention(q[l, b, h * G:(h + 1) * G].reshape(G * Tq, d), K, V, vis.reshape(G * Tq, -1), 1 / np.sqrt(d))
         got = o[l, b, h * G:(h + 1) * G].reshape(G * Tq, d)
-        bound = ref.attention_bound(want, E, S, n + m, d, dtype, G * Tq > 16)
+        bound = ref.attention_bound(want, E, S, n + m, d, dtype, kb.kvev_debug_page_form(sh, c.pages, Tq)[0] > 16)
         bad = ~(np.abs(got - want) <= bound)
         assert not bad.any(), (what, (l, b, h), np.argwhere(bad)[:4], got[bad][:4], want[bad][:4], bound[bad][:4])
 
@@ -238,13 +238,31 @@ CASES = [  # dtype, d, page, L, B, H, Hkv, lengths, Tq, causal, k_cap
 ]
 
 
-@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c)).replace(" ", ""))
-def test_attention(case):
+FRAMES = [
+    ("bf16", 128, 16, 1, 1, 48, 1, [1], 1, False, 0),
+    ("bf16", 128, 64, 1, 2, 4, 4, [700, 65], 50, True, 0),
+    ("bf16", 64, 16, 2, 2, 4, 2, [0, 130], 24, False, 0),
+    ("bf16", 128, 32, 1, 3, 8, 2, [90, 2, 257], 33, True, 70),
+    ("bf16", 64, 256, 1, 1, 4, 1, [900], 33, True, 5),
+    ("bf16", 128, 64, 2, 1, 8, 2, [333], 100, False, 0),
+    ("bf16", 64, 128, 1, 2, 2, 1, [640, 130], 130, True, 0),
+    ("bf16", 128, 16, 1, 2, 6, 2, [400, 70], 90, True, 17),
+    ("bf16", 128, 128, 1, 1, 4, 2, [1000], 150, True, 17),
+    ("bf16", 128, 32, 1, 2, 4, 2, [0, 45], 200, False, 130),
+    ("bf16", 128, 64, 1, 1, 4, 1, [2050], 64, False, 0),
+    ("bf16", 64, 32, 1, 1, 2, 1, [1500], 300, True, 200),
+]
+
+
+def attention_case(case, form=None):
     name, d, page, L, B, H, Hkv, lengths, Tq, causal, k_cap = case
     dtype = torch.float32 if name == "f32" else torch.bfloat16
     for T in {0, max(lengths), 1}:
         sh = shape_of(L, B, H, Hkv, d, dtype, T)
         c = cache_of(sh, page, lengths, Tq=Tq)
+        if form:
+            queries, runs = kb.kvev_debug_page_form(sh, c.pages, Tq)
+            assert queries == form
         fill(c, lengths, dtype)
         Q = normal(7, L, B, H, Tq, d, dtype=dtype)
         O = torch.full_like(Q, 9.0)
@@ -262,12 +280,55 @@ def test_attention(case):
         kb.kvev_page_attention(sh, c.pages, Q, Tq, c.pool, c.table, c.length, again, c.ws_attn, None, ints(q_start) if causal else None,
                                *(store or (None, None, None)), k_cap)
         assert torch.equal(O, again)                     # the same bits, and the tickets are zero again
-        head = c.ws_attn[:4 * L * B * Hkv]
-        assert not head.any()
+        assert not c.ws_attn[:4 * L * B * Hkv].any()
+
+
+@pytest.fixture
+def frames():
+    """Small shapes walk the frame kernels too."""
+    kb.kvev_debug_page_frame_work(1)
+    yield
+    kb.kvev_debug_page_frame_work(0)
+
+
+@pytest.fixture
+def streamed():
+    """Rows are read with the non-temporal hint."""
+    kb.kvev_debug_attn_stream_bytes(1)
+    yield
+    kb.kvev_debug_attn_stream_bytes(0)
+
+
+def case_id(c):
+    return "-".join(map(str, c)).replace(" ", "")
+
+
+@pytest.mark.parametrize("case", CASES, ids=case_id)
+def test_attention(case):
+    attention_case(case, 16)
+
+
+@pytest.mark.parametrize("case", CASES[::4], ids=case_id)
+def test_attention_streamed(case, streamed):
+    attention_case(case, 16)
+
+
+@pytest.mark.parametrize("case", FRAMES, ids=case_id)
+def test_attention_of_frames(case, frames):
+    attention_case(case, 128 if case[5] // case[6] * case[8] <= 128 else 256)
+
+
+def test_attention_forms():
+    """What a call's work makes of it."""
+    pages = kb.make_pages(64, 1 << 12, 128)
+    for (B, Hkv, G, Tq, T), (queries, runs) in {(16, 8, 4, 256, 8192): (256, 1), (16, 8, 4, 4, 8192): (16, 8), (1, 8, 4, 256, 4000): (256, 8), (1, 8, 4, 256, 600): (16, 1),
+                                                (16, 8, 4, 32, 4000): (128, 4), (1, 32, 1, 1, 4091): (16, 8), (64, 8, 4, 1, 8192): (16, 2), (1, 32, 1, 1, 300): (16, 1)}.items():
+        assert kb.kvev_debug_page_form(shape_of(1, B, Hkv * G, Hkv, T=T), pages, Tq) == (queries, runs), (B, Hkv, G, Tq, T)
+    assert kb.kvev_debug_page_form(shape_of(1, 16, 32, 8, T=8192, dtype=torch.float32), pages, 256)[0] == 16
 
 
 @pytest.mark.parametrize("Tq", [1, 40])
-def test_attention_over_a_window(Tq):
+def test_attention_over_a_window(Tq, frames):
     """Tokens before `first` and pages given up; entries that are no page inside the window; lengths that are wrong."""
     sh, lengths, first = shape_of(B=4, H=4, H_kv=2), [300, 200, 150, 90], [100, 64, 149, 90]
     c = cache_of(sh, 32, lengths[:3] + [96], Tq=Tq)
@@ -288,7 +349,7 @@ def test_attention_over_a_window(Tq):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("Tq", [1, 30])
-def test_attention_keeps_what_is_hidden_apart(dtype, Tq):
+def test_attention_keeps_what_is_hidden_apart(dtype, Tq, frames):
     """Blocks that are not finite: in hidden tokens they change nothing, in seen ones a key spoils the query, a value its block."""
     n = 150
     sh = shape_of(B=2, H=4, H_kv=2, dtype=dtype)
@@ -311,24 +372,25 @@ def test_attention_keeps_what_is_hidden_apart(dtype, Tq):
     assert torch.isnan(O[:, 1, 2:4]).all()
 
 
-def test_attention_scores_of_every_size():
+@pytest.mark.parametrize("dtype,Tq", [(torch.float32, 1), (torch.bfloat16, 1), (torch.bfloat16, 60)])
+def test_attention_scores_of_every_size(dtype, Tq, frames):
     """Keys and queries so large that all weight is on one token, and so small that it is shared alike."""
-    sh, n = shape_of(B=2, H=2, dtype=torch.float32), 200
+    sh, n = shape_of(B=2, H=2, dtype=dtype), 200
     for scale in (1e-20, 30.0, 1e15):
-        K = normal(1, 1, 2, 2, n, 128, dtype=torch.float32) * scale
-        c = cache_of(sh, 16, [n, n])
-        fill(c, [n, n], torch.float32, K=K)
-        Q = normal(3, 1, 2, 2, 1, 128, dtype=torch.float32)
+        K = (normal(1, 1, 2, 2, n, 128, dtype=torch.float32) * scale).to(dtype)
+        c = cache_of(sh, 16, [n, n], Tq=Tq)
+        fill(c, [n, n], dtype, K=K)
+        Q = normal(3, 1, 2, 2, Tq, 128, dtype=dtype)
         O = torch.empty_like(Q)
-        c.attend(Q, 1, O)
+        c.attend(Q, Tq, O)
         assert torch.isfinite(O).all()
         if scale < 1e10:
             check_attention(c, Q, O, [n, n])
         else:                                    # all weight on one token: scores are 1e12 and more apart
             k, v = torch.empty_like(K), torch.empty_like(K)
             c.read(ints([0, 0]), None, n, k, v)
-            best = torch.matmul(k.double(), Q.double().transpose(3, 4).contiguous()).squeeze(-1).argmax(-1)
-            assert torch.equal(O[..., 0, :], torch.gather(v, 3, best[..., None, None].expand(-1, -1, -1, 1, 128)).squeeze(3))
+            best = torch.matmul(k.double(), Q.double().transpose(3, 4).contiguous()).argmax(3)
+            assert torch.equal(O, torch.gather(v, 3, best[..., None].expand(-1, -1, -1, -1, 128)))
 
 
 def test_attention_of_a_long_cache():
