@@ -113,7 +113,7 @@ static int rows_common(const kvev_shape *sh, const kvev_pages *pg, const void *K
     if (rc) return rc;
     if (!whole16(K) || !whole16(V) || !whole16(pool) || !aligned4(table) || !aligned4(start) || !aligned4_or_null(n_new) || Tn < 0)
         return KVEV_ERR_INVALID_ARG;
-    if ((int64_t)sh->L * sh->B * a->g.Hkv * Tn > INT32_MAX) return KVEV_ERR_INVALID_ARG;
+    if ((int64_t)sh->L * sh->B * a->g.Hkv * Tn > INT32_MAX) return KVEV_ERR_INVALID_ARG;      // (a workgroup or less each)
     a->pool = static_cast<unsigned char *>(pool); a->table = table; a->start = start; a->n_new = n_new; a->Tn = Tn;
     return KVEV_OK;
 }
@@ -339,6 +339,7 @@ int kvev_pages_compact(const kvev_shape *sh, const kvev_pages *pg, const void *p
     a.pool = static_cast<unsigned char *>(const_cast<void *>(pool)); a.table = const_cast<int32_t *>(table); a.refs = const_cast<int32_t *>(refs);
     a.to_pool = static_cast<unsigned char *>(to_pool); a.to_table = to_table; a.to_refs = to_refs; a.to_pages = t.n_pages;
     a.status = status; a.ws = static_cast<int32_t *>(ws);
+    a.stream = std::min(pool_bytes(a.g), pool_bytes(t)) > attn_stream_bytes();
     const hipError_t e = launch_pages_compact(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? KVEV_OK : hip_fail(e);
 }

@@ -144,39 +144,43 @@ __global__ __launch_bounds__(1024) void reserve_kernel(PagesArgs a)
     }
 }
 
-// 16-byte pieces from one place to another by a workgroup
-__device__ __forceinline__ void copy_pieces(unsigned char *to, const unsigned char *from, size_t bytes)
+// 16-byte pieces from one place to another by NT threads, of which this is number i.  STREAM: with the non-temporal hint, for more
+// than the caches hold.
+template <int NT, bool STREAM> __device__ __forceinline__ void copy_pieces(unsigned char *to, const unsigned char *from, size_t bytes, int i0)
 {
     u32x4_t *y = reinterpret_cast<u32x4_t *>(to);
     const u32x4_t *x = reinterpret_cast<const u32x4_t *>(from);
     const int64_t n = (int64_t)(bytes / 16);
     constexpr int U = 4;
-    for (int64_t i = threadIdx.x; i < n; i += 256 * U) {
+    for (int64_t i = i0; i < n; i += NT * U) {
         u32x4_t v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i + 256 * u < n) v[u] = x[i + 256 * u];
+            if (i + NT * u < n) v[u] = STREAM ? __builtin_nontemporal_load(x + i + NT * u) : x[i + NT * u];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i + 256 * u < n) {
-                y[i + 256 * u] = v[u];
+            if (i + NT * u < n) {
+                if (STREAM) __builtin_nontemporal_store(v[u], y + i + NT * u);
+                else y[i + NT * u] = v[u];
                 hold_store_data(v[u]);
             }
     }
 }
 
-// the groups in use of every page that a row shared and goes on in
+// The groups in use of every page that a row shared and goes on in: a wave to a (row, layer, head), since most have a few groups of
+// 2 KiB (15 rows x 32 layers x 8 heads, one group each: 9.2 us by a workgroup each).
 __global__ __launch_bounds__(256) void reserve_copy_kernel(PagesArgs a)
 {
     const PageGeom &g = a.g;
     const int32_t *rows = a.ws + kHead;
     const int64_t units = (int64_t)a.ws[0] * g.L * g.Hkv;
     const size_t block = block_bytes(g);
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int h = (int)(u % g.Hkv), l = (int)(u / g.Hkv % g.L), b = rows[kTo * g.B + (int)(u / g.Hkv / g.L)];
+    for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += (int64_t)gridDim.x * 4) {
+        const int64_t ml = u / g.Hkv;
+        const int h = (int)(u - ml * g.Hkv), i = (int)(ml / g.L), l = (int)(ml - (int64_t)i * g.L), b = rows[kTo * g.B + i];
         const size_t from = rows[kNeed * g.B + b], to = rows[kAt * g.B + b], base = (size_t)l * g.n_pages;
-        copy_pieces(a.pool + ((base + to) * g.Hkv + h) * block, a.pool + ((base + from) * g.Hkv + h) * block,
-                    (size_t)rows[kGroups * g.B + b] * group_bytes(g.d));
+        copy_pieces<64, false>(a.pool + ((base + to) * g.Hkv + h) * block, a.pool + ((base + from) * g.Hkv + h) * block,
+                               (size_t)rows[kGroups * g.B + b] * group_bytes(g.d), threadIdx.x & 63);
     }
 }
 
@@ -255,7 +259,8 @@ __global__ __launch_bounds__(256) void copy_kernel(PagesArgs a)
             if (!ok && threadIdx.x == 0) atomicOr(a.status, kStatusPair);
         }
         if (!ok) continue;
-        copy_pieces(a.pool + ((size_t)l * g.n_pages + dst) * g.Hkv * block, a.pool + ((size_t)l * g.n_pages + src) * g.Hkv * block, g.Hkv * block);
+        copy_pieces<256, false>(a.pool + ((size_t)l * g.n_pages + dst) * g.Hkv * block, a.pool + ((size_t)l * g.n_pages + src) * g.Hkv * block,
+                                g.Hkv * block, threadIdx.x);
     }
 }
 
@@ -292,7 +297,7 @@ __global__ __launch_bounds__(1024) void compact_rank_kernel(PagesArgs a)
     for (int p = used + threadIdx.x; p < a.to_pages; p += 1024) a.to_refs[p] = 0;
 }
 
-__global__ __launch_bounds__(256) void compact_copy_kernel(PagesArgs a)
+template <bool STREAM> __global__ __launch_bounds__(256) void compact_copy_kernel(PagesArgs a)
 {
     if (!a.ws[0]) return;
     const PageGeom &g = a.g;
@@ -306,7 +311,8 @@ __global__ __launch_bounds__(256) void compact_copy_kernel(PagesArgs a)
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
         const int l = (int)(u / g.n_pages), p = (int)(u - (int64_t)l * g.n_pages), to = rank[p];
         if (to < 0) continue;
-        copy_pieces(a.to_pool + ((size_t)l * a.to_pages + to) * g.Hkv * block, a.pool + ((size_t)l * g.n_pages + p) * g.Hkv * block, g.Hkv * block);
+        copy_pieces<256, STREAM>(a.to_pool + ((size_t)l * a.to_pages + to) * g.Hkv * block, a.pool + ((size_t)l * g.n_pages + p) * g.Hkv * block,
+                                 g.Hkv * block, threadIdx.x);
     }
 }
 
@@ -317,7 +323,7 @@ hipError_t launch_pages_reserve(const PagesArgs &a, hipStream_t st)
     hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(1024), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(reserve_copy_kernel, dim3(grid_of((int64_t)a.g.B * a.g.L * a.g.Hkv, 2048)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(reserve_copy_kernel, dim3(grid_of(((int64_t)a.g.B * a.g.L * a.g.Hkv + 3) / 4, 2048)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 hipError_t launch_pages_fork(const PagesArgs &a, hipStream_t st)
@@ -340,7 +346,9 @@ hipError_t launch_pages_compact(const PagesArgs &a, hipStream_t st)
     hipLaunchKernelGGL(compact_rank_kernel, dim3(1), dim3(1024), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(compact_copy_kernel, dim3(grid_of((int64_t)a.g.n_pages * a.g.L, 2048)), dim3(256), 0, st, a);
+    const dim3 grid(grid_of((int64_t)a.g.n_pages * a.g.L, 2048));
+    if (a.stream) hipLaunchKernelGGL((compact_copy_kernel<true>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((compact_copy_kernel<false>), grid, dim3(256), 0, st, a);
     return hipGetLastError();
 }
 

@@ -73,6 +73,7 @@ struct PagesArgs {
     unsigned char *to_pool;       // compact
     int32_t *to_table, *to_refs;
     int to_pages;
+    int stream;                   // compact: as in PageAttnArgs
 };
 
 hipError_t launch_rotary(const RotaryArgs &a, int dtype, hipStream_t st);
