@@ -73,8 +73,9 @@ int kvev_debug_attn_stream_bytes(size_t bytes);
 int kvev_debug_page_frame_work(int64_t work);
 
 /* How a kvev_page_attention call would run: queries of a unit (16; a frame's 128
- * or 256) and the most workgroups that share a unit's rows.  Errors: INVALID_ARG. */
-int kvev_debug_page_form(const kvev_shape *shape, const kvev_pages *pages, int Tq, int *queries, int *runs);
+ * or 256), waves of a workgroup and the most workgroups that share a unit's rows.
+ * Errors: INVALID_ARG. */
+int kvev_debug_page_form(const kvev_shape *shape, const kvev_pages *pages, int Tq, int *queries, int *waves, int *runs);
 
 /* Calibration of the memory system for the benchmark's roofline notes (bench.py
  * --calibrate-stream): a plain streaming kernel, one workgroup per tile, reads

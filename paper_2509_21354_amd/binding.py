@@ -127,7 +127,7 @@ def lib() -> ctypes.CDLL:
         L.kvev_debug_decode_queries.restype = ci
         L.kvev_debug_page_frame_work.argtypes = [ctypes.c_int64]
         L.kvev_debug_page_frame_work.restype = ci
-        L.kvev_debug_page_form.argtypes = [shp, ctypes.POINTER(Pages), ci, ctypes.POINTER(ci), ctypes.POINTER(ci)]
+        L.kvev_debug_page_form.argtypes = [shp, ctypes.POINTER(Pages), ci, ctypes.POINTER(ci), ctypes.POINTER(ci), ctypes.POINTER(ci)]
         L.kvev_debug_page_form.restype = ci
         L.kvev_debug_lstm_form.argtypes = [shp, ci, ctypes.POINTER(ci)]
         L.kvev_debug_lstm_form.restype = ci
@@ -252,11 +252,11 @@ def kvev_debug_page_frame_work(work: int = 0) -> None:
     _check(lib().kvev_debug_page_frame_work(work), "kvev_debug_page_frame_work")
 
 
-def kvev_debug_page_form(shape: Shape, pages: "Pages", Tq: int) -> Tuple[int, int]:
-    queries, runs = ctypes.c_int(), ctypes.c_int()
-    st = lib().kvev_debug_page_form(ctypes.byref(shape), ctypes.byref(pages), Tq, ctypes.byref(queries), ctypes.byref(runs))
+def kvev_debug_page_form(shape: Shape, pages: "Pages", Tq: int) -> Tuple[int, int, int]:
+    queries, waves, runs = ctypes.c_int(), ctypes.c_int(), ctypes.c_int()
+    st = lib().kvev_debug_page_form(ctypes.byref(shape), ctypes.byref(pages), Tq, ctypes.byref(queries), ctypes.byref(waves), ctypes.byref(runs))
     _check(st, "kvev_debug_page_form")
-    return queries.value, runs.value
+    return queries.value, waves.value, runs.value
 
 
 def kvev_debug_lstm_fused_min_groups(min_groups: int = 0) -> None:

@@ -42,26 +42,29 @@ static size_t elem(const kvev_shape *sh) { return sh->dtype == KVEV_F32 ? 4 : 2;
 static size_t pool_bytes(const PageGeom &g) { return (size_t)g.L * g.n_pages * page_bytes(g); }
 
 // ---- attention over pages: planning ----
-// A unit is 16 queries of a key-value head; its rows, in chunks of 64 (one for each of a workgroup's 4 waves in turn), are cut into
-// runs of `run` chunks, a workgroup each.  A batch row takes as many of a unit's nsplit workgroups as its own length pays for
+// A unit is 16 queries of a key-value head; its rows, in chunks of 64 for one wave each, are cut into runs of `run` chunks, a
+// workgroup of 1, 4 or 8 waves each.  A batch row takes as many of a unit's nsplit workgroups as its own length pays for
 // (decided on the device, where the lengths are).  shape->T, or the capacity if it is 0, says for which length the launch is made;
-// results depend on it in the order of sums only.
-//   * Runs of 4 chunks and more, so that the units take one workgroup per compute unit: 32 units x 4091 tokens 11.4 us, with two or
-//     four per compute unit 13.0; 8 units x 16000 tokens 14.7 and 20 us.
-//   * Up to 8 chunks one run: 32 x 300 tokens 7.6 us, in two runs 8.5; 8 units x 500 tokens 7.5 and 7.8 us.  (32 x 1000: 8.8 us in
-//     runs of 4, 10.4 in runs of 8.)
-//   * Where such a run would be longer than 16 chunks, runs for four workgroups per compute unit, of 16 chunks at least: they hide
-//     each other's ends, and long rows of a ragged batch are spread (32 x 16000 tokens 19.9 us, one workgroup per compute unit 22.0;
-//     512 units of 64 ragged rows up to 8192 tokens 63 us, unsplit 72; 128 units of 16 ragged rows up to 12000 29 and 47 us).
-// Frames (page_frame.hip; bf16): units of 128 or 256 queries, two workgroups or one per compute unit, runs of 4 chunks and more so
-// that one round of workgroups fills the chip.  They take calls with 48 queries or more to a key-value head and enough work
+// results depend on it in the order of sums and the choice of form only.
+//   * While runs of 8 chunks are no more than the compute units: 8 waves, a chunk each (us, 8 and 4 waves: 32 units x 300 tokens 7.3 and
+//     8.0, x 1000 9.9 and 10.9, x 4091 11.2 and 11.8; 64 units x 2000 10.7 and 11.1; 8 units x 16000 13.8 and 15.3).  More runs,
+//     or longer ones, are worse: 512 units x 400 tokens 13.1 and 9.9.  fp32, whose registers leave no room for more waves than
+//     that, takes them up to one unit per compute unit (256 units x 2000 tokens 19.9 and 23.0).
+//   * Many units of short rows: a wave each, which has no other wave to wait for and whose beginning others hide (2048 units x 320
+//     tokens 19.5, with 4 waves 24.7; x 1000 49.3 and 53.7; 16384 x 320 116 and 156; but x 8192 383 and 358, and 512 units x
+//     320 12.4 and 8.9).
+//   * Else 4 waves, in runs that give every compute unit one, of 4 chunks at least; where such a run would be longer than 16 chunks, in
+//     runs for four workgroups per compute unit, of 16 chunks at least: they hide each other's ends, and long rows of a ragged
+//     batch are spread (32 x 16000 tokens 19.9 us, one workgroup per compute unit 22.0; 512 units of 64 ragged rows up to 8192
+//     tokens 63, unsplit 72; 128 units of 16 ragged rows up to 12000 29 and 47).
+// Frames (page_frame.hip; bf16): units of 128 or 256 queries, two workgroups or one per compute unit.  They take calls with 48 queries or more to a key-value head and enough work
 // (units of 16 queries x tokens; 4 query heads to a key-value head, units of 16 and frame, us): 128 heads x 64 queries x 4000
 // tokens 54.2 and 52.6; 128 x 128 x 600 24.2 and 26.0; 128 x 256 x 600 34.7 and 33.9; 512 x 64 x 600 40.8 and 32.6; 8 x 1024 x
 // 4000 47.8 and 41.8; but 8 x 1024 x 600 12.9 and 23.5, 8 x 256 x 4000 19.9 and 34.4, and 512 x 32 x 4000 106 and 124.
-constexpr int kPageChunk = 64, kPageMaxSplit = 64, kFrameQueries = 48;
+constexpr int kPageChunk = 64, kPageMaxSplit = 64, kFrameQueries = 48, kFrameRounds = 3;
 constexpr int64_t kFrameWork = 1200000;
 static std::atomic<int64_t> g_frame_work{kFrameWork};      // (kvev_debug_page_frame_work lowers it)
-struct PageAttnPlan { int queries, qtiles, nsplit, run; int64_t units; size_t ticket_bytes, ws_bytes, ws_any; };
+struct PageAttnPlan { int queries, waves, qtiles, nsplit, run; int64_t units; size_t ticket_bytes, ws_bytes, ws_any; };
 static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int Tq, int64_t tokens, bool frame)
 {
     PageAttnPlan p;
@@ -70,8 +73,33 @@ static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int 
     p.qtiles = (int)((R + p.queries - 1) / p.queries);
     p.units = (int64_t)g.L * g.B * g.Hkv * p.qtiles;
     const int64_t chunks = (tokens + kPageChunk - 1) / kPageChunk, slots = p.queries == 128 ? 2 * cus : cus;
-    int64_t run = std::max<int64_t>((chunks * p.units + slots - 1) / slots, !frame && chunks <= 8 ? 8 : 4);
-    if (!frame && run > 16) run = std::max<int64_t>(16, (chunks * p.units + 4 * slots - 1) / (4 * slots));
+    auto fill = [&](int64_t wgs) { return (chunks * p.units + wgs - 1) / wgs; };       // the run of which `wgs` workgroups take all
+    int64_t run;
+    if (frame) {
+        p.waves = p.queries / 32;
+        // as many runs as give the least time: rounds of workgroups, each run two tiles longer for its beginning and end, a tile of
+        // 64 rows 2.2 us (d = 128, 256 queries), partials out and in at 4 TB/s and a launch
+        const double tile = 2.2 * g.d / 128, merge = 2.0 * p.queries * (g.d + 4) * sizeof(float) / 4e6;
+        double least = 0;
+        int64_t best = 1;
+        for (int64_t n = 1; n <= std::min<int64_t>(kPageMaxSplit, (chunks + 3) / 4) && (n == 1 || p.units * n <= kFrameRounds * slots); ++n) {
+            const double rounds = (double)((p.units * n + slots - 1) / slots);
+            const double t = rounds * ((double)((chunks + n - 1) / n) + 2) * tile + (n > 1 ? 4 + merge * (double)(p.units * n) : 0.0);
+            if (n == 1 || t < least) { least = t; best = n; }
+        }
+        run = (chunks + best - 1) / best;
+    } else if (sh->dtype == KVEV_F32 ? p.units <= cus : p.units * ((chunks + 7) / 8) <= cus) {
+        p.waves = 8;
+        const int64_t n = std::max<int64_t>(cus / p.units, 1);
+        run = std::max<int64_t>((chunks + n - 1) / n, 8);
+    } else if (p.units >= 6 * cus && chunks <= 32) {
+        p.waves = 1;
+        run = chunks;
+    } else {
+        p.waves = 4;
+        run = std::max<int64_t>(fill(cus), 4);
+        if (run > 16) run = std::max<int64_t>(fill(4 * cus), 16);
+    }
     run = std::min(std::max(run, (chunks + kPageMaxSplit - 1) / kPageMaxSplit), std::max<int64_t>(chunks, 1));
     p.run = (int)run;
     p.nsplit = (int)std::max<int64_t>(1, (chunks + run - 1) / run);
@@ -82,7 +110,7 @@ static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int 
     p.ws_bytes = scratch(p.nsplit);
     // enough for every length of row: a unit takes no more than its share of the workgroups wanted (rounded up), and no run is
     // shorter than 4 chunks
-    const int64_t wanted = frame ? slots : 4 * slots;
+    const int64_t wanted = frame ? kFrameRounds * slots : 4 * slots;
     p.ws_any = scratch(std::min<int64_t>({kPageMaxSplit, (wanted + p.units - 1) / p.units, (cap / kPageChunk + 4) / 4}));
     return p;
 }
@@ -131,12 +159,13 @@ int kvev_debug_page_frame_work(int64_t work)
     return KVEV_OK;
 }
 
-int kvev_debug_page_form(const kvev_shape *sh, const kvev_pages *pg, int Tq, int *queries, int *runs)
+int kvev_debug_page_form(const kvev_shape *sh, const kvev_pages *pg, int Tq, int *queries, int *waves, int *runs)
 {
     PageGeom g;
-    if (check_pages(sh, pg, &g) != KVEV_OK || Tq < 1 || !queries || !runs) return KVEV_ERR_INVALID_ARG;
+    if (check_pages(sh, pg, &g) != KVEV_OK || Tq < 1 || !queries || !waves || !runs) return KVEV_ERR_INVALID_ARG;
     const PageAttnPlan p = plan_page_attn(sh, g, Tq, plan_tokens(sh, g));
     *queries = p.queries;
+    *waves = p.waves;
     *runs = p.nsplit;
     return KVEV_OK;
 }
@@ -249,7 +278,7 @@ int kvev_page_attention(const kvev_shape *sh, const kvev_pages *pg, const void *
     }
     a.stream = (size_t)sh->L * sh->B * a.g.Hkv * (size_t)plan_tokens(sh, a.g) * 17 * sh->d / 16 > attn_stream_bytes();
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)sh->d));
-    const hipError_t e = p.queries == 16 ? launch_page_attention(a, sh->dtype, static_cast<hipStream_t>(stream))
+    const hipError_t e = p.queries == 16 ? launch_page_attention(a, sh->dtype, p.waves, static_cast<hipStream_t>(stream))
                                          : launch_page_frame(a, p.queries, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? KVEV_OK : hip_fail(e);
 }

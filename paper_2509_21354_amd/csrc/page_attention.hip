@@ -22,6 +22,7 @@
 // at the end.
 #include "kernels.hpp"
 #include "pages.hpp"
+#include <atomic>
 #include <utility>
 
 namespace kvev {
@@ -110,15 +111,19 @@ template <int D> __device__ __forceinline__ int turn_of(int t)
     return D == 128 ? (t & 7) << 1 | (t >> 3 & 1) : (t >> 1 & 3) << 1 | (t >> 3 & 1);
 }
 
-template <typename T, int D, bool STREAM>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_kernel(PageAttnArgs a)
+// bytes of LDS of a wave: its staging rows, then its outputs
+template <int D> constexpr int wave_lds() { return 32 * D * 2 > 16 * (D + 4) * 4 ? 32 * D * 2 : 16 * (D + 4) * 4; }
+
+template <typename T, int D, int NW, bool STREAM>
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void page_attention_kernel(PageAttnArgs a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int NQ = Terms<T>::Q, NP = Terms<T>::P, KS = D / 32, DT = D / 16, NB = D / 32;
     constexpr int OP = D + 4;                    // pitch of the waves' outputs
-    constexpr int STAGE = 32 * D * 2, OUT = 16 * OP * 4;
-    __shared__ __align__(256) unsigned char s_mem[4 * (STAGE > OUT ? STAGE : OUT)];
-    __shared__ float s_m[4][16], s_l[4][16];
+    constexpr int STAGE = 32 * D * 2;
+    extern __shared__ __align__(256) unsigned char s_mem[];
+    // maxima and sums of the waves; of the 16 rows of threads in the last merge
+    __shared__ float s_m[NW][16], s_l[NW][16];
 
     const PageGeom &g = a.g;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -136,10 +141,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) Terms<T>::load(static_cast<const T *>(a.Q) + orow * D + gr * (D / 4) + kk * 8, qf[kk]);
 
-    // Lane 4 j + i holds the table's entry for group i of this wave's chunk j (of 16): asked for before the length is there, as if
+    // Lane 4 j + i holds the table's entry for group i of this wave's chunk j (of 16; its chunks lie NW apart): asked for before the length is there, as if
     // the rows were the pages' from the beginning on and the run as long as planned, which they are most of the time.
     const int32_t *table = a.table + (size_t)b * g.max_pages;
-    const uint32_t ahead = (uint32_t)((lane >> 2) * 256 + (lane & 3) * 16);
+    const uint32_t ahead = (uint32_t)((lane >> 2) * (64 * NW) + (lane & 3) * 16);
     auto entry = [&](uint32_t t) __attribute__((always_inline)) { return table[min((t + ahead) >> g.page_shift, (uint32_t)g.max_pages - 1u)]; };
     const uint32_t guess = ((uint32_t)split * (uint32_t)a.run + (uint32_t)wave) * 64u;
     int pv = entry(guess);
@@ -242,7 +247,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
 
     // ---- rows of the store ----
     int ch = c0 + wave;
-    for (; ch < min(sc, c1); ch += 4) {
+    for (; ch < min(sc, c1); ch += NW) {
         f32x4_t st[4];
         bf16x8_t pb[2][NP];
         const T *Kc = static_cast<const T *>(a.Kc) + (size_t)s * a.k_cap * D, *Vc = static_cast<const T *>(a.Vc) + (size_t)s * a.k_cap * D;
@@ -285,11 +290,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
 
     // ---- tokens of the pages ----
     const int tok = base0 + (ch - sc) * 64;      // the first of this wave's chunks
-    const int mine = ch < c1 ? (c1 - ch + 3) >> 2 : 0;
+    const int mine = ch < c1 ? (c1 - ch + NW - 1) / NW : 0;
     if ((uint32_t)tok != guess) pv = entry((uint32_t)tok);
     // the pages of chunks j0 .. j0 + 15 from their entries; -1: none
     auto checked = [&](int e, int j0) __attribute__((always_inline)) {
-        const uint32_t pi = ((uint32_t)tok + (uint32_t)j0 * 256u + ahead) >> g.page_shift;
+        const uint32_t pi = ((uint32_t)tok + (uint32_t)j0 * (64u * NW) + ahead) >> g.page_shift;
         return j0 + (lane >> 2) < mine && pi < (uint32_t)g.max_pages && (uint32_t)e < (uint32_t)g.n_pages ? e : -1;
     };
     typedef typename Codes<D>::type codes_t;
@@ -298,9 +303,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
     uint32_t sk[4], sv[4];                       // scale bytes: of the key, of the value in the byte above
     const unsigned char *vbase[4];
     pv = checked(pv, 0);
-    int pv_next = entry((uint32_t)tok + 16u * 256u);
+    int pv_next = entry((uint32_t)tok + 16u * (64u * NW));
     auto fetch_keys = [&](int j) __attribute__((always_inline)) {
-        const int t0 = tok + j * 256;
+        const int t0 = tok + j * (64 * NW);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int page = max(__builtin_amdgcn_readlane(pv, (j & 15) * 4 + i), 0);
@@ -320,7 +325,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
         fetch_values();
     }
     for (int j = 0; j < mine; ++j) {
-        const int t0 = tok + j * 256;
+        const int t0 = tok + j * (64 * NW);
         const uint64_t none = __ballot(pv < 0);
         const uint32_t gone = (uint32_t)(none >> ((j & 15) * 4)) & 15u;       // groups without a page
         const bool full = gone == 0 && t0 >= first && t0 + 64 <= len && t0 + 63 <= lim_all;
@@ -345,7 +350,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
         if (j + 1 < mine) {
             if ((j + 1) % 16 == 0) {
                 pv = checked(pv_next, j + 1);
-                pv_next = entry((uint32_t)tok + (uint32_t)(j + 17) * 256u);
+                pv_next = entry((uint32_t)tok + (uint32_t)(j + 17) * (64u * NW));
             }
             fetch_keys(j + 1);
         }
@@ -396,19 +401,19 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t *>(s_o + (wave * 16 + n) * OP + dt * 16 + 4 * gr) = o[dt];
     __syncthreads();
-    constexpr int EPT = D / 16;                  // elements of a thread: 16 threads per query, their elements 16 apart
-    const int oq = tid >> 4, oe = tid & 15, orr = qt * 16 + oq;
+    constexpr int TPQ = 4 * NW, EPT = D / TPQ;   // threads per query, and their elements, TPQ apart
+    const int oq = tid / TPQ, oe = tid % TPQ, orr = qt * 16 + oq;
     float M = s_m[0][oq];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) M = fmaxf(M, s_m[w][oq]);
+    for (int w = 1; w < NW; ++w) M = fmaxf(M, s_m[w][oq]);
     const float Mr = M == -INFINITY ? 0.f : M;
     float L = 0.f, acc[EPT] = {};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
         const float f = __builtin_amdgcn_exp2f(s_m[w][oq] - Mr);
         L += s_l[w][oq] * f;
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) acc[e] += s_o[(w * 16 + oq) * OP + oe + 16 * e] * f;
+        for (int e = 0; e < EPT; ++e) acc[e] += s_o[(w * 16 + oq) * OP + oe + TPQ * e] * f;
     }
     // where query q of the unit's output begins
     auto out_of = [&](int q) __attribute__((always_inline)) {
@@ -420,14 +425,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
             const float inv = 1.0f / L;                          // (no rows: 0 below; a NaN stays one)
             T *O = out_of(oq);
 #pragma unroll
-            for (int e = 0; e < EPT; ++e) Storage<T>::store(O + oe + 16 * e, L == 0.f ? 0.f : acc[e] * inv);
+            for (int e = 0; e < EPT; ++e) Storage<T>::store(O + oe + TPQ * e, L == 0.f ? 0.f : acc[e] * inv);
         }
         return;
     }
     if (orr < R) {
         float *part = a.part + (((size_t)unit * a.nsplit + split) * 16 + oq) * (D + 2);
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) store_device(part + oe + 16 * e, acc[e]);
+        for (int e = 0; e < EPT; ++e) store_device(part + oe + TPQ * e, acc[e]);
         if (oe == 0) { store_device(part + D, M); store_device(part + D + 1, L); }
     }
     // ---- the workgroups meet: as in decode attention ----
@@ -456,7 +461,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
             const float px = load_device(pp + D), pl = load_device(pp + D + 1);
             float v[EPT];
 #pragma unroll
-            for (int e = 0; e < EPT; ++e) v[e] = load_device(pp + oe + 16 * e);
+            for (int e = 0; e < EPT; ++e) v[e] = load_device(pp + oe + TPQ * e);
             const float Mn = fmaxf(M, px), ref = Mn == -INFINITY ? 0.f : Mn, f0 = __builtin_amdgcn_exp2f(M - ref), f1 = __builtin_amdgcn_exp2f(px - ref);
             L = L * f0 + pl * f1;
 #pragma unroll
@@ -469,7 +474,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
         float *mm = &s_m[0][0], *ll = &s_l[0][0];
         if (oe == 0) { mm[oq] = M; ll[oq] = L; }
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) s_o[oq * OP + oe + 16 * e] = acc[e];
+        for (int e = 0; e < EPT; ++e) s_o[oq * OP + oe + TPQ * e] = acc[e];
         __syncthreads();
         if (k0 != 0) return;
         M = -INFINITY;
@@ -482,34 +487,46 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void page_attention_ke
             const float f = __builtin_amdgcn_exp2f(mm[q + Q * k] - ref);
             L += ll[q + Q * k] * f;
 #pragma unroll
-            for (int e = 0; e < EPT; ++e) acc[e] += s_o[(q + Q * k) * OP + oe + 16 * e] * f;
+            for (int e = 0; e < EPT; ++e) acc[e] += s_o[(q + Q * k) * OP + oe + TPQ * e] * f;
         }
     }
     if (q >= live) return;
     T *O = out_of(q);
     const float inv = 1.0f / L;
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) Storage<T>::store(O + oe + 16 * e, L == 0.f ? 0.f : acc[e] * inv);
+    for (int e = 0; e < EPT; ++e) Storage<T>::store(O + oe + TPQ * e, L == 0.f ? 0.f : acc[e] * inv);
 #endif
 }
 
-template <typename T, int D> static void launch_page_attention_as(const PageAttnArgs &a, dim3 grid, hipStream_t st)
+template <typename T, int D, int NW, bool STREAM> static hipError_t launch_waves(const PageAttnArgs &a, hipStream_t st)
 {
-    if (a.stream) hipLaunchKernelGGL((page_attention_kernel<T, D, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((page_attention_kernel<T, D, false>), grid, dim3(256), 0, st, a);
+    constexpr int lds = NW * wave_lds<D>();
+    if (lds > 64 * 1024 - 2048) {
+        static std::atomic<uint64_t> done{0};
+        const hipError_t e = allow_lds(page_attention_kernel<T, D, NW, STREAM>, lds, done);
+        if (e != hipSuccess) return e;
+    }
+    const dim3 grid((unsigned)((int64_t)a.g.L * a.g.B * a.g.Hkv * a.qtiles * a.nsplit));
+    hipLaunchKernelGGL((page_attention_kernel<T, D, NW, STREAM>), grid, dim3(64 * NW), lds, st, a);
+    return hipGetLastError();
+}
+template <typename T, int D, bool STREAM> static hipError_t launch_stream(const PageAttnArgs &a, int waves, hipStream_t st)
+{
+    switch (waves) {
+    case 1: return launch_waves<T, D, 1, STREAM>(a, st);
+    case 4: return launch_waves<T, D, 4, STREAM>(a, st);
+    default: return launch_waves<T, D, 8, STREAM>(a, st);
+    }
+}
+template <typename T> static hipError_t launch_type(const PageAttnArgs &a, int waves, hipStream_t st)
+{
+    if (a.g.d == 128) return a.stream ? launch_stream<T, 128, true>(a, waves, st) : launch_stream<T, 128, false>(a, waves, st);
+    return a.stream ? launch_stream<T, 64, true>(a, waves, st) : launch_stream<T, 64, false>(a, waves, st);
 }
 
-hipError_t launch_page_attention(const PageAttnArgs &a, int dtype, hipStream_t st)
+hipError_t launch_page_attention(const PageAttnArgs &a, int dtype, int waves, hipStream_t st)
 {
-    const dim3 grid((unsigned)((int64_t)a.g.L * a.g.B * a.g.Hkv * a.qtiles * a.nsplit));
-    if (dtype == KVEV_F32) {
-        if (a.g.d == 128) launch_page_attention_as<float, 128>(a, grid, st);
-        else launch_page_attention_as<float, 64>(a, grid, st);
-    } else {
-        if (a.g.d == 128) launch_page_attention_as<bf16_t, 128>(a, grid, st);
-        else launch_page_attention_as<bf16_t, 64>(a, grid, st);
-    }
-    return hipGetLastError();
+    return dtype == KVEV_F32 ? launch_type<float>(a, waves, st) : launch_type<bf16_t>(a, waves, st);
 }
 
 }  // namespace kvev

@@ -6,8 +6,8 @@
 // the token and not on the head, so a thread makes those of its pairs once and takes them through the heads of its slice;
 // queries and keys of one call are one list of heads.  Bytes bound it, sine and cosine where a token has few heads: 64 rows x 256
 // tokens x (32 + 8) heads, bf16, d = 128: 65 us, 5.2 TB/s in and out, what a copy of that size reaches.  Where the pairs are no
-// multiple of a piece, halves pay for the ends of pieces element by element (4 x 1000 x 64 heads, 61 pairs: 51 us, 60 pairs
-// neighbouring 23 us).  Tried and dropped: non-temporal accesses (no difference); ends in halves and quarters of a piece (scratch: 76 us).
+// multiple of a piece, halves pay for the ends of pieces element by element (4 x 1000 x 64 heads, 61 pairs: 51 us, as
+// neighbouring pairs 23 us).  Tried and dropped: non-temporal accesses (no difference); ends in halves and quarters of a piece (scratch: 76 us).
 #include "kernels.hpp"
 #include "pages.hpp"
 

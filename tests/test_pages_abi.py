@@ -177,6 +177,16 @@ def test_python_calls_say_what_is_wrong_with_a_tensor():
     assert c.pool.numel() == 348160 and (c.table == -1).all() and not c.refs.any()
 
 
+def test_hooks():
+    L, n = kb.lib(), ctypes.c_int()
+    assert L.kvev_debug_page_frame_work(-1) == kb.ERR_INVALID_ARG and L.kvev_debug_page_frame_work(0) == kb.OK
+    sh, pg, r = _shape(), kb.make_pages(32, 10, 7), ctypes.byref(n)
+    f = L.kvev_debug_page_form
+    assert f(ctypes.byref(sh), ctypes.byref(pg), 1, r, r, r) == kb.OK
+    assert f(ctypes.byref(sh), ctypes.byref(pg), 0, r, r, r) == kb.ERR_INVALID_ARG and f(ctypes.byref(sh), ctypes.byref(pg), 1, None, r, r) == kb.ERR_INVALID_ARG
+    assert f(ctypes.byref(sh), ctypes.byref(kb.make_pages(31, 10, 7)), 1, r, r, r) == kb.ERR_INVALID_ARG
+
+
 def test_plain_form_of_the_cache():
     """The tests' plain form against itself: codes are nearest, halfway cases go to the even one, blocks that are not finite are lost."""
     import numpy as np

@@ -261,8 +261,7 @@ def attention_case(case, form=None):
         sh = shape_of(L, B, H, Hkv, d, dtype, T)
         c = cache_of(sh, page, lengths, Tq=Tq)
         if form:
-            queries, runs = kb.kvev_debug_page_form(sh, c.pages, Tq)
-            assert queries == form
+            assert kb.kvev_debug_page_form(sh, c.pages, Tq)[0] == form
         fill(c, lengths, dtype)
         Q = normal(7, L, B, H, Tq, d, dtype=dtype)
         O = torch.full_like(Q, 9.0)
@@ -318,12 +317,35 @@ def test_attention_of_frames(case, frames):
     attention_case(case, 128 if case[5] // case[6] * case[8] <= 128 else 256)
 
 
+@pytest.mark.parametrize("dtype,L,B,Hkv,G,Tq,T,form", [
+    (torch.bfloat16, 16, 12, 8, 2, 3, 150, (16, 1, 1)), (torch.bfloat16, 4, 24, 8, 1, 1, 600, (16, 4, 1)), (torch.float32, 16, 12, 8, 1, 1, 150, (16, 1, 1)),
+    (torch.float32, 1, 33, 8, 2, 2, 200, (16, 4, 1)), (torch.bfloat16, 1, 2, 8, 1, 1, 3000, (16, 8, 6)), (torch.bfloat16, 1, 16, 8, 1, 1, 3000, (16, 4, 3))])
+def test_attention_by_waves(dtype, L, B, Hkv, G, Tq, T, form):
+    """Workgroups of 1, 4 and 8 waves: ragged rows, a window, a store, tokens that see those before them."""
+    lengths = [T if b == 0 else (T * ((37 * b) % B)) // B for b in range(B)]
+    sh = shape_of(L, B, Hkv * G, Hkv, 64, dtype, T)
+    c = cache_of(sh, 32, lengths, Tq=Tq)
+    assert kb.kvev_debug_page_form(sh, c.pages, Tq) == form
+    fill(c, lengths, dtype)
+    Q = normal(7, L, B, Hkv * G, Tq, 64, dtype=dtype)
+    O = torch.full_like(Q, 9.0)
+    store = (normal(8, L, B, Hkv, 9, 64, dtype=dtype), normal(9, L, B, Hkv, 9, 64, dtype=dtype), torch.full((L, B, Hkv), 7, dtype=I32, device="cuda"))
+    first, q_start = [n // 3 for n in lengths], [n - Tq for n in lengths]
+    rng = random.Random(T)
+    heads = [(rng.randrange(L), b, rng.randrange(Hkv)) for b in range(B)]
+    c.attend(Q, Tq, O)
+    check_attention(c, Q, O, lengths, heads=heads)
+    kb.kvev_page_attention(sh, c.pages, Q, Tq, c.pool, c.table, c.length, O, c.ws_attn, ints(first), ints(q_start), *store, 9)
+    check_attention(c, Q, O, lengths, first, q_start, store, heads)
+
+
 def test_attention_forms():
     """What a call's work makes of it."""
     pages = kb.make_pages(64, 1 << 12, 128)
-    for (B, Hkv, G, Tq, T), (queries, runs) in {(16, 8, 4, 256, 8192): (256, 1), (16, 8, 4, 4, 8192): (16, 8), (1, 8, 4, 256, 4000): (256, 8), (1, 8, 4, 256, 600): (16, 1),
-                                                (16, 8, 4, 32, 4000): (128, 4), (1, 32, 1, 1, 4091): (16, 8), (64, 8, 4, 1, 8192): (16, 2), (1, 32, 1, 1, 300): (16, 1)}.items():
-        assert kb.kvev_debug_page_form(shape_of(1, B, Hkv * G, Hkv, T=T), pages, Tq) == (queries, runs), (B, Hkv, G, Tq, T)
+    for (B, Hkv, G, Tq, T), form in {(16, 8, 4, 256, 8192): (256, 8, 1), (16, 8, 4, 4, 8192): (16, 4, 8), (1, 8, 4, 256, 4000): (256, 8, 8),
+                                     (1, 8, 4, 256, 600): (16, 4, 1), (16, 8, 4, 32, 4000): (128, 4, 4), (1, 32, 1, 1, 4091): (16, 8, 8), (64, 8, 4, 1, 8192): (16, 4, 2),
+                                     (1, 32, 1, 1, 300): (16, 8, 1), (64, 32, 1, 1, 1000): (16, 1, 1), (64, 32, 1, 1, 8192): (16, 4, 1)}.items():
+        assert kb.kvev_debug_page_form(shape_of(1, B, Hkv * G, Hkv, T=T), pages, Tq) == form, (B, Hkv, G, Tq, T)
     assert kb.kvev_debug_page_form(shape_of(1, 16, 32, 8, T=8192, dtype=torch.float32), pages, 256)[0] == 16
 
 
