@@ -328,7 +328,7 @@ size_t kvev_page_pool_bytes(const kvev_shape *shape, const kvev_pages *pages);
 size_t kvev_page_workspace_bytes(int op, const kvev_shape *shape, const kvev_pages *pages, int n);
 
 /* New rows into the pages: K, V [L,B,H_kv,Tn,d]; row t < n_new[b] of batch row b becomes
- * token start[b] + t (n_new NULL: all Tn; more than Tn count as Tn).  Nothing is written for
+ * token start[b] + t (n_new NULL: all Tn; more than Tn count as Tn; L * B * H_kv * Tn <= 2^30).  Nothing is written for
  * a batch row with start[b] < 0, nor for tokens past the capacity or without a page.  Tokens
  * that are there may be written again.  No two rows of a call may name the same token of the
  * same page.  Does not look at lengths: kvev_pages_reserve makes room, moves them on and gives `start`. */
@@ -348,7 +348,8 @@ int kvev_page_read(const kvev_shape *shape, const kvev_pages *pages, const void 
  * the tokens [first[b], length[b]) of the pages (first NULL: from 0).  q_start NULL: every
  * query sees all of them.  Else query i is token q_start[b] + i and sees those up to itself;
  * with q_start as kvev_pages_reserve gives it, the queries are the tokens just appended.  (In
- * a padded batch, queries from n_new[b] on get some finite output that means nothing.)  Tokens without a
+ * a padded batch, queries from n_new[b] on get an output that means nothing, and so do those of a row whose
+ * start is -1.)  Tokens without a
  * page are left out.  A query that sees no row gives zeros.
  * Scores, softmax and sums are fp32, O is rounded once.  fp32: operands enter the matrix
  * cores as three bf16 terms; bf16: the softmax weights as two, 16 significant bits, or as one
@@ -369,7 +370,7 @@ int kvev_page_attention(const kvev_shape *shape, const kvev_pages *pages, const 
  * order, lowest index first, a row's copy before its new pages.  If there are not enough for all,
  * nothing changes but start = -1 throughout and KVEV_PAGES_NONE_FREE; a row past its capacity or without its
  * last page is left alone with start = -1 and KVEV_PAGES_BAD_ROW.  (kvev_page_append skips rows
- * whose start is -1.)  n_new, length and start are three arrays.  Workspace:
+ * whose start is -1.)  n_new, length and start must not overlap.  Workspace:
  * KVEV_OP_PAGES_RESERVE, written by every call. */
 int kvev_pages_reserve(const kvev_shape *shape, const kvev_pages *pages, const int32_t *n_new, int32_t *table,
                        int32_t *length, int32_t *refs, void *pool, int32_t *start, int32_t *status, void *ws,

@@ -122,6 +122,7 @@ static PageAttnPlan plan_page_attn(const kvev_shape *sh, const PageGeom &g, int 
     f.ws_any = p.ws_any = std::max(p.ws_any, f.ws_any);      // (the form depends on the length as well)
     return p.units * tokens >= g_frame_work.load() ? f : p;
 }
+static bool page_queries_fit(const kvev_shape *sh, int Tq) { return (int64_t)sh->L * sh->B * sh->H * Tq <= (int64_t)1 << 26; }
 static int64_t plan_tokens(const kvev_shape *sh, const PageGeom &g)
 {
     const int64_t cap = (int64_t)g.max_pages << g.page_shift;
@@ -141,7 +142,7 @@ static int rows_common(const kvev_shape *sh, const kvev_pages *pg, const void *K
     if (rc) return rc;
     if (!whole16(K) || !whole16(V) || !whole16(pool) || !aligned4(table) || !aligned4(start) || !aligned4_or_null(n_new) || Tn < 0)
         return KVEV_ERR_INVALID_ARG;
-    if ((int64_t)sh->L * sh->B * a->g.Hkv * Tn > INT32_MAX) return KVEV_ERR_INVALID_ARG;      // (a workgroup or less each)
+    if ((int64_t)sh->L * sh->B * a->g.Hkv * Tn > (int64_t)1 << 30) return KVEV_ERR_INVALID_ARG;
     a->pool = static_cast<unsigned char *>(pool); a->table = table; a->start = start; a->n_new = n_new; a->Tn = Tn;
     return KVEV_OK;
 }
@@ -162,7 +163,7 @@ int kvev_debug_page_frame_work(int64_t work)
 int kvev_debug_page_form(const kvev_shape *sh, const kvev_pages *pg, int Tq, int *queries, int *waves, int *runs)
 {
     PageGeom g;
-    if (check_pages(sh, pg, &g) != KVEV_OK || Tq < 1 || !queries || !waves || !runs) return KVEV_ERR_INVALID_ARG;
+    if (check_pages(sh, pg, &g) != KVEV_OK || Tq < 1 || !page_queries_fit(sh, Tq) || !queries || !waves || !runs) return KVEV_ERR_INVALID_ARG;
     const PageAttnPlan p = plan_page_attn(sh, g, Tq, plan_tokens(sh, g));
     *queries = p.queries;
     *waves = p.waves;
@@ -182,7 +183,7 @@ size_t kvev_page_workspace_bytes(int op, const kvev_shape *sh, const kvev_pages 
     if (check_pages(sh, pg, &g) != KVEV_OK || n < 0) return 0;
     switch (op) {
     case KVEV_OP_PAGE_ATTENTION:
-        return n == 0 ? 0 : plan_page_attn(sh, g, n, plan_tokens(sh, g)).ws_any;
+        return n == 0 || !page_queries_fit(sh, n) ? 0 : plan_page_attn(sh, g, n, plan_tokens(sh, g)).ws_any;
     case KVEV_OP_PAGES_RESERVE:
         return reserve_words(g) * 4;
     case KVEV_OP_PAGES_COMPACT:
@@ -264,7 +265,7 @@ int kvev_page_attention(const kvev_shape *sh, const kvev_pages *pg, const void *
     if (k_cap > 0 && (!whole16(Kc) || !whole16(Vc) || !aligned4(count))) return KVEV_ERR_INVALID_ARG;
     if ((int64_t)sh->L * sh->B * a.g.Hkv * k_cap > INT32_MAX) return KVEV_ERR_INVALID_ARG;
     if (Tq == 0) return KVEV_OK;
-    if ((int64_t)sh->L * sh->B * sh->H * Tq > (int64_t)1 << 26) return KVEV_ERR_INVALID_ARG;
+    if (!page_queries_fit(sh, Tq)) return KVEV_ERR_INVALID_ARG;
     const size_t q_bytes = (size_t)sh->L * sh->B * sh->H * Tq * sh->d * elem(sh);
     if (overlap(Q, q_bytes, O, q_bytes)) return KVEV_ERR_INVALID_ARG;
     const PageAttnPlan p = plan_page_attn(sh, a.g, Tq, plan_tokens(sh, a.g));
@@ -292,7 +293,9 @@ int kvev_pages_reserve(const kvev_shape *sh, const kvev_pages *pg, const int32_t
     if (rc) return rc;
     rc = check_tables(a.g, table, length, refs);
     if (rc) return rc;
-    if (!aligned4(n_new) || !aligned4(start) || !aligned4(status) || !whole16(pool) || n_new == length || start == length || start == n_new)
+    if (!aligned4(n_new) || !aligned4(start) || !aligned4(status) || !whole16(pool)) return KVEV_ERR_INVALID_ARG;
+    const size_t row_bytes = (size_t)sh->B * 4;
+    if (overlap(n_new, row_bytes, length, row_bytes) || overlap(start, row_bytes, length, row_bytes) || overlap(start, row_bytes, n_new, row_bytes))
         return KVEV_ERR_INVALID_ARG;
     if (!whole16(ws) || ws_bytes < reserve_words(a.g) * 4) return KVEV_ERR_WORKSPACE;
     a.n_new = n_new; a.table = table; a.length = length; a.refs = refs; a.pool = static_cast<unsigned char *>(pool);

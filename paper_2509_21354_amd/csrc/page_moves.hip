@@ -246,21 +246,18 @@ __global__ __launch_bounds__(256) void copy_kernel(PagesArgs a)
 {
     const PageGeom &g = a.g;
     const size_t block = block_bytes(g);
-    const int64_t units = (int64_t)a.n * g.L;
-    int last = -1;
-    bool ok = false;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int i = (int)(u / g.L), l = (int)(u - (int64_t)i * g.L), src = a.src[i], dst = a.dst[i];
-        if (i != last) {                   // (as in fork_kernel)
-            last = i;
-            ok = (uint32_t)src < (uint32_t)g.n_pages && (uint32_t)dst < (uint32_t)g.n_pages;
-            ok = !among(a.dst, i, dst) && ok;
-            ok = !among(a.dst, a.n, src) && ok;
-            if (!ok && threadIdx.x == 0) atomicOr(a.status, kStatusPair);
+    for (int i = blockIdx.x; i < a.n; i += gridDim.x) {
+        const int src = a.src[i], dst = a.dst[i];
+        bool ok = (uint32_t)src < (uint32_t)g.n_pages && (uint32_t)dst < (uint32_t)g.n_pages;        // (as in fork_kernel)
+        ok = !among(a.dst, i, dst) && ok;
+        ok = !among(a.dst, a.n, src) && ok;
+        if (!ok) {
+            if (threadIdx.x == 0) atomicOr(a.status, kStatusPair);
+            continue;
         }
-        if (!ok) continue;
-        copy_pieces<256, false>(a.pool + ((size_t)l * g.n_pages + dst) * g.Hkv * block, a.pool + ((size_t)l * g.n_pages + src) * g.Hkv * block,
-                                g.Hkv * block, threadIdx.x);
+        for (int l = blockIdx.y; l < g.L; l += gridDim.y)
+            copy_pieces<256, false>(a.pool + ((size_t)l * g.n_pages + dst) * g.Hkv * block, a.pool + ((size_t)l * g.n_pages + src) * g.Hkv * block,
+                                    g.Hkv * block, threadIdx.x);
     }
 }
 
@@ -338,7 +335,8 @@ hipError_t launch_pages_trim(const PagesArgs &a, hipStream_t st)
 }
 hipError_t launch_pages_copy(const PagesArgs &a, hipStream_t st)
 {
-    hipLaunchKernelGGL(copy_kernel, dim3(grid_of((int64_t)a.n * a.g.L, 2048)), dim3(256), 0, st, a);
+    const unsigned pages = grid_of(a.n, 2048), layers = grid_of(a.g.L, (2048 + pages - 1) / pages);
+    hipLaunchKernelGGL(copy_kernel, dim3(pages, layers), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 hipError_t launch_pages_compact(const PagesArgs &a, hipStream_t st)

@@ -126,7 +126,6 @@ static hipError_t launch_rotary_as(const RotaryArgs &a, hipStream_t st)
     slices = slices < want ? slices : want;
     if (slices < 1) slices = 1;
     const int64_t blocks = (int64_t)a.B * ttiles * slices;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks), block(256);
     if (a.adjacent) hipLaunchKernelGGL((rotary_kernel<T, true>), grid, block, 0, st, a, slots, tb, ttiles, (int)slices);
     else hipLaunchKernelGGL((rotary_kernel<T, false>), grid, block, 0, st, a, slots, tb, ttiles, (int)slices);

@@ -102,7 +102,8 @@ def test_overlaps():
     assert _call("attention", Tq=1, Q=_far(0), O=_far(0) + 256) == kb.ERR_INVALID_ARG
     assert _call("read", Tn=4, K=_far(0), V=_far(0) + 256) == kb.ERR_INVALID_ARG
     assert _call("reserve", n_new=FAKE, start=FAKE) == kb.ERR_INVALID_ARG and _call("reserve", start=_far(0)) == kb.ERR_INVALID_ARG
-    assert _call("reserve", n_new=_far(0)) == kb.ERR_INVALID_ARG
+    assert _call("reserve", n_new=_far(0)) == kb.ERR_INVALID_ARG and _call("reserve", start=_far(0) + 8) == kb.ERR_INVALID_ARG
+    assert _call("reserve", n_new=_far(1) - 4) == kb.ERR_INVALID_ARG
     assert _call("compact", to_pool=_far(0) + 64) == kb.ERR_INVALID_ARG and _call("compact", to_refs=_far(2) + 4) == kb.ERR_INVALID_ARG
     assert _call("compact", to_table=_far(1) + 4) == kb.ERR_INVALID_ARG
     for kw in (dict(Q_out=_far(0) + 16), dict(K_out=_far(1) + 16), dict(K_out=_far(2)), dict(K_out=_far(0)), dict(Q_out=_far(1))):
@@ -123,6 +124,7 @@ def test_workspaces():
     for T in (1, 64, 1000, 6400):
         sh.T = sh.T_cap = T
         assert kb.page_workspace_bytes(kb.OP_PAGE_ATTENTION, sh, pg, 1) == need
+    assert kb.page_workspace_bytes(kb.OP_PAGE_ATTENTION, sh, pg, 1 << 30) == 0
     assert kb.page_workspace_bytes(99, sh, pg, 1) == 0 and kb.page_workspace_bytes(kb.OP_PAGE_ATTENTION, sh, pg, -1) == 0
     assert kb.page_workspace_bytes(kb.OP_PAGE_ATTENTION, sh, kb.make_pages(17, 1, 1), 1) == 0
 

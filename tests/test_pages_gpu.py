@@ -544,6 +544,10 @@ def test_compact(n_pages, max_pages, B, page):
             assert int(t.status) == kb.PAGES_NONE_FREE and (t.pool == 77).all() and (t.table == -5).all() and (t.refs == -5).all()
             continue
         rank = {p: i for i, p in enumerate(live)}
+        own = c.table.clone()                     # the table may be rewritten in place
+        again = [torch.empty_like(x) for x in (t.pool, t.refs)]
+        kb.kvev_pages_compact(sh, c.pages, c.pool, own, c.refs, t.pages, again[0], own, again[1], t.status, ws)
+        assert torch.equal(own, t.table) and torch.equal(again[1], t.refs)
         assert int(t.status) == 0 and t.refs.tolist() == [int(refs[p]) for p in live] + [0] * (room - len(live))
         assert t.table.tolist() == [[rank.get(int(p), -1) for p in row] for row in table]
         x, y = c.pool.view(2, n_pages, -1), t.pool.view(2, room, -1)
@@ -631,7 +635,8 @@ def test_a_decode_step_in_a_graph():
     Qs, Ks, Vs = (normal(i, N, L, B, h, 1, d) for i, h in enumerate((H, 2, 2)))
 
     def run(graphs):
-        c = kb.PagedCache(sh, page, 30, 6)
+        c = kb.PagedCache(sh, page, 30, 200)                # (planned for 3200 tokens: rows may be cut into several runs)
+        assert kb.kvev_debug_page_form(sh, c.pages, 1)[2] > 1
         Q, K, V, O = Qs[0].clone(), Ks[0].clone(), Vs[0].clone(), torch.empty_like(Qs[0])
         one, outs = ints([1, 1, 0]), []
 
@@ -662,6 +667,31 @@ def test_a_decode_step_in_a_graph():
         assert c.length.tolist() == [N, N, 0] and int(c.status) == 0
         return torch.stack(outs)
     assert torch.equal(run(False), run(True))
+
+
+def test_frames_in_a_graph(frames):
+    """A frame captured before any other ran, in runs that a second launch merges; its graph replayed as the cache grows."""
+    sh, page, Tq = shape_of(1, 2, 8, 1, 64), 16, 10
+    c = kb.PagedCache(sh, page, 100, 50, Tq)
+    assert kb.kvev_debug_page_form(sh, c.pages, Tq)[0] == 128 and kb.kvev_debug_page_form(sh, c.pages, Tq)[2] > 1
+    K, V, Q = (normal(i, 3, 1, 2, h, 300, 64) for i, h in enumerate((1, 1, 8)))
+    O, want = torch.empty(1, 2, 8, Tq, 64, dtype=torch.bfloat16, device="cuda"), None
+    q = Q[0, :, :, :, :Tq].contiguous()
+    c.reserve(ints([300, 7]))
+    c.append(K[0], V[0], 300, ints([300, 7]))
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.attend(q, Tq, O)
+    for i in range(3):
+        if i:
+            c.reserve(ints([200, 3]))
+            c.append(K[i, ..., :200, :].contiguous(), V[i, ..., :200, :].contiguous(), 200, ints([200, 3]))
+        g.replay()
+        want = torch.empty_like(O)
+        c.attend(q, Tq, want)
+        assert torch.equal(O, want)
+        check_attention(c, q, O, c.length.tolist())
 
 
 def test_calls_on_another_stream():
