@@ -81,8 +81,8 @@ __global__ __launch_bounds__(1024) void reserve_kernel(PagesArgs a)
     // the free pages of lowest index
     int found = 0;
     constexpr int PER = 8;
-    for (int p0 = 0; found < total && p0 < g.n_pages; p0 += 1024 * PER) {
-        const int p = p0 + tid * PER;
+    for (int64_t p0 = 0; found < total && p0 < g.n_pages; p0 += 1024 * PER) {
+        const int64_t p = p0 + tid * PER;
         int free_bits = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(1024) void reserve_kernel(PagesArgs a)
 #pragma unroll
         for (int i = 0; i < PER; ++i)
             if (free_bits >> i & 1) {
-                if (at < total) list[at] = p + i;
+                if (at < total) list[at] = (int)p + i;
                 ++at;
             }
         found += sum;
@@ -269,8 +269,8 @@ __global__ __launch_bounds__(1024) void compact_rank_kernel(PagesArgs a)
     int32_t *rank = a.ws + kHead;
     int used = 0;
     constexpr int PER = 8;
-    for (int p0 = 0; p0 < g.n_pages; p0 += 1024 * PER) {
-        const int p = p0 + threadIdx.x * PER;
+    for (int64_t p0 = 0; p0 < g.n_pages; p0 += 1024 * PER) {
+        const int64_t p = p0 + (int)threadIdx.x * PER;
         int bits = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
