@@ -327,11 +327,12 @@ size_t kvev_page_pool_bytes(const kvev_shape *shape, const kvev_pages *pages);
  * kvev_page_attention, else unused. */
 size_t kvev_page_workspace_bytes(int op, const kvev_shape *shape, const kvev_pages *pages, int n);
 
-/* New rows into the pages: K, V [L,B,H_kv,Tn,d]; row t < n_new[b] of batch row b becomes
- * token start[b] + t (n_new NULL: all Tn; more than Tn count as Tn; L * B * H_kv * Tn <= 2^30).  Nothing is written for
- * a batch row with start[b] < 0, nor for tokens past the capacity or without a page.  Tokens
- * that are there may be written again.  No two rows of a call may name the same token of the
- * same page.  Does not look at lengths: kvev_pages_reserve makes room, moves them on and gives `start`. */
+/* New rows into the pages: K, V [L,B,H_kv,Tn,d]; row t < n_new[b] of batch row b becomes token
+ * start[b] + t (n_new NULL: all Tn; more than Tn count as Tn; L * B * H_kv * Tn <= 2^30).
+ * Nothing is written for a batch row with start[b] < 0, nor for tokens past the capacity or
+ * without a page.  Tokens that are there may be written again.  No two rows of a call may name
+ * the same token of the same page.  Does not look at lengths: kvev_pages_reserve makes room,
+ * moves them on and gives `start`. */
 int kvev_page_append(const kvev_shape *shape, const kvev_pages *pages, const void *K, const void *V, int Tn,
                      const int32_t *start, const int32_t *n_new, const int32_t *table, void *pool, void *stream);
 
@@ -342,44 +343,44 @@ int kvev_page_append(const kvev_shape *shape, const kvev_pages *pages, const voi
 int kvev_page_read(const kvev_shape *shape, const kvev_pages *pages, const void *pool, const int32_t *table,
                    const int32_t *first, const int32_t *n, int Tn, void *K, void *V, void *stream);
 
-/* Eq. 1 over the pages: the queries Q [L,B,H,Tq,d] of batch row b attend, per key-value
- * head, to rows 0 .. count - 1 of a compact store as kvev_retain leaves it (Kc, Vc
- * [L,B,H_kv,k_cap,d], count [L,B,H_kv]; k_cap = 0: none, the pointers may be NULL) and to
- * the tokens [first[b], length[b]) of the pages (first NULL: from 0).  q_start NULL: every
- * query sees all of them.  Else query i is token q_start[b] + i and sees those up to itself;
- * with q_start as kvev_pages_reserve gives it, the queries are the tokens just appended.  (In
- * a padded batch, queries from n_new[b] on get an output that means nothing, and so do those of a row whose
- * start is -1.)  Tokens without a
- * page are left out.  A query that sees no row gives zeros.
- * Scores, softmax and sums are fp32, O is rounded once.  fp32: operands enter the matrix
- * cores as three bf16 terms; bf16: the softmax weights as two, 16 significant bits, or as one
- * rounded to bf16 in frames (48 queries or more to a key-value head, and enough rows to pay for the
- * form), whose normaliser sums them unrounded as in kvev_gated_attention.  shape->T (0: the
- * capacity) says for what length of row the launch is made; any length is right, and results
- * depend on it in the order of sums and the choice of the form only.
- * Workspace: kvev_page_workspace_bytes(KVEV_OP_PAGE_ATTENTION, shape, pages, Tq), enough for
- * every T; zero-filled before its first use, tickets as in kvev_gated_attention.  O must not overlap Q. */
+/* Eq. 1 over the pages: the queries Q [L,B,H,Tq,d] of batch row b attend, per key-value head, to
+ * rows 0 .. count - 1 of a compact store as kvev_retain leaves it (Kc, Vc [L,B,H_kv,k_cap,d],
+ * count [L,B,H_kv]; k_cap = 0: none, the pointers may be NULL) and to the tokens [first[b],
+ * length[b]) of the pages (first NULL: from 0).  q_start NULL: every query sees all of them.
+ * Else query i is token q_start[b] + i and sees those up to itself; with q_start as
+ * kvev_pages_reserve gives it, the queries are the tokens just appended.  (In a padded batch,
+ * queries from n_new[b] on get an output that means nothing, and so do those of a row whose start
+ * is -1.)  Tokens without a page are left out.  A query that sees no row gives zeros.
+ * Scores, softmax and sums are fp32, O is rounded once.  fp32: operands enter the matrix cores as
+ * three bf16 terms; bf16: the softmax weights as two, 16 significant bits, or as one rounded to
+ * bf16 in frames (48 queries or more to a key-value head, and enough rows to pay for the form),
+ * whose normaliser sums them unrounded as in kvev_gated_attention.  shape->T (0: the capacity)
+ * says for what length of row the launch is made; any length is right, and results depend on it
+ * in the order of sums and the choice of the form only.
+ * Workspace: kvev_page_workspace_bytes(KVEV_OP_PAGE_ATTENTION, shape, pages, Tq), enough for every
+ * T and for fewer queries; zero-filled before its first use, tickets as in kvev_gated_attention.
+ * Calls of any Tq and T may take the same one, one after the other.  O must not overlap Q. */
 int kvev_page_attention(const kvev_shape *shape, const kvev_pages *pages, const void *Q, int Tq, const void *pool,
                         const int32_t *table, const int32_t *length, const int32_t *first, const int32_t *q_start,
                         const void *Kc, const void *Vc, const int32_t *count, int k_cap, void *O, void *ws,
                         size_t ws_bytes, void *stream);
 
-/* Room for n_new[b] >= 0 more tokens in every batch row: missing pages are taken, start[b] =
- * the old length, length[b] += n_new[b].  A row that goes on in a page which others hold as
- * well gets a copy of it first (of what it has in use).  Free pages go to rows in ascending
- * order, lowest index first, a row's copy before its new pages.  If there are not enough for all,
- * nothing changes but start = -1 throughout and KVEV_PAGES_NONE_FREE; a row past its capacity or without its
- * last page is left alone with start = -1 and KVEV_PAGES_BAD_ROW.  (kvev_page_append skips rows
- * whose start is -1.)  n_new, length and start must not overlap.  Workspace:
+/* Room for n_new[b] >= 0 more tokens in every batch row: missing pages are taken, start[b] = the
+ * old length, length[b] += n_new[b].  A row that goes on in a page which others hold as well gets
+ * a copy of it first (of what it has in use).  Free pages go to rows in ascending order, lowest
+ * index first, a row's copy before its new pages.  If there are not enough for all, nothing
+ * changes but start = -1 throughout and KVEV_PAGES_NONE_FREE; a row past its capacity or without
+ * its last page is left alone with start = -1 and KVEV_PAGES_BAD_ROW.  (kvev_page_append skips
+ * rows whose start is -1.)  n_new, length and start must not overlap.  Workspace:
  * KVEV_OP_PAGES_RESERVE, written by every call. */
 int kvev_pages_reserve(const kvev_shape *shape, const kvev_pages *pages, const int32_t *n_new, int32_t *table,
                        int32_t *length, int32_t *refs, void *pool, int32_t *start, int32_t *status, void *ws,
                        size_t ws_bytes, void *stream);
 
-/* Batch row dst[i] (empty: length 0) becomes a second holder of row src[i]'s pages and length,
- * i < n <= B.  No keys or values move: kvev_pages_reserve copies a shared page when a row writes on in
- * it.  A pair is refused (KVEV_PAGES_BAD_PAIR, the others go ahead) if a row is outside [0, B),
- * if dst[i] is not empty or stands in an earlier pair, or if src[i] is some pair's dst. */
+/* Batch row dst[i] (empty: length 0) becomes a second holder of row src[i]'s pages and length, i
+ * < n <= B.  No keys or values move: kvev_pages_reserve copies a shared page when a row writes on
+ * in it.  A pair is refused (KVEV_PAGES_BAD_PAIR, the others go ahead) if a row is outside [0,
+ * B), if dst[i] is not empty or stands in an earlier pair, or if src[i] is some pair's dst. */
 int kvev_pages_fork(const kvev_shape *shape, const kvev_pages *pages, const int32_t *src, const int32_t *dst, int n,
                     int32_t *table, int32_t *length, int32_t *refs, int32_t *status, void *stream);
 
@@ -397,11 +398,12 @@ int kvev_pages_trim(const kvev_shape *shape, const kvev_pages *pages, const int3
 int kvev_pages_copy(const kvev_shape *shape, const kvev_pages *pages, void *pool, const int32_t *src,
                     const int32_t *dst, int n, int32_t *status, void *stream);
 
-/* The pages in use (refs > 0), in ascending order, into the first pages of another pool, which may
- * be smaller (to->n_pages; to->page and to->max_pages as in `pages`): to_pool, to_table
- * [B, max_pages] (may be table itself), to_refs [to->n_pages].  Pages of to_pool behind them are left as
- * they were, their counts are 0.  If there are too few, nothing is written but KVEV_PAGES_NONE_FREE.  The pools and the
- * counts must not overlap.  Workspace: KVEV_OP_PAGES_COMPACT of the source. */
+/* The pages in use (refs > 0), in ascending order, into the first pages of another pool, which
+ * may be smaller (to->n_pages; to->page and to->max_pages as in `pages`): to_pool, to_table [B,
+ * max_pages] (may be table itself), to_refs [to->n_pages].  Pages of to_pool behind them are left
+ * as they were, their counts are 0.  If there are too few, nothing is written but
+ * KVEV_PAGES_NONE_FREE.  The pools and the counts must not overlap.  Workspace:
+ * KVEV_OP_PAGES_COMPACT of the source. */
 int kvev_pages_compact(const kvev_shape *shape, const kvev_pages *pages, const void *pool, const int32_t *table,
                        const int32_t *refs, const kvev_pages *to, void *to_pool, int32_t *to_table, int32_t *to_refs,
                        int32_t *status, void *ws, size_t ws_bytes, void *stream);

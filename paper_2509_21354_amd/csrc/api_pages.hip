@@ -103,15 +103,16 @@ static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int 
     run = std::min(std::max(run, (chunks + kPageMaxSplit - 1) / kPageMaxSplit), std::max<int64_t>(chunks, 1));
     p.run = (int)run;
     p.nsplit = (int)std::max<int64_t>(1, (chunks + run - 1) / run);
-    // tickets, then the partials of every run: 16 queries' outputs, maxima and sums, or the waves' of a frame as they hold them
-    p.ticket_bytes = ((size_t)p.units * sizeof(int32_t) + 255) / 256 * 256;
+    // Tickets, then the partials of every run: 16 queries' outputs, maxima and sums, or the waves' of a frame as they hold them.
+    // One ticket per unit of 16 queries that is split; four workgroups per compute unit bound their number, and room for as many
+    // stands first whatever the call: the partials of one call then never lie where another one has its tickets.
+    p.ticket_bytes = ((size_t)4 * cus * sizeof(int32_t) + 255) / 256 * 256;
     const size_t partial = (!frame ? (size_t)16 * (g.d + 2) : (size_t)p.queries * (g.d + 4)) * sizeof(float);
-    auto scratch = [&](int64_t n) { return n > 1 ? p.ticket_bytes + (size_t)p.units * n * partial : (size_t)0; };
-    p.ws_bytes = scratch(p.nsplit);
-    // enough for every length of row: a unit takes no more than its share of the workgroups wanted (rounded up), and no run is
-    // shorter than 4 chunks
-    const int64_t wanted = frame ? kFrameRounds * slots : 4 * slots;
-    p.ws_any = scratch(std::min<int64_t>({kPageMaxSplit, (wanted + p.units - 1) / p.units, (cap / kPageChunk + 4) / 4}));
+    p.ws_bytes = p.nsplit > 1 ? p.ticket_bytes + (size_t)p.units * p.nsplit * partial : 0;
+    // enough for every length of row and for fewer queries: split units take the workgroups wanted (rounded up to the unit), and no
+    // run is shorter than 4 chunks
+    const int64_t wanted = frame ? kFrameRounds * slots : 4 * slots, units = std::min(p.units, wanted), most = (cap / kPageChunk + 4) / 4;
+    p.ws_any = most > 1 ? p.ticket_bytes + (size_t)std::min({units * kPageMaxSplit, units + wanted, units * most}) * partial : 0;
     return p;
 }
 static PageAttnPlan plan_page_attn(const kvev_shape *sh, const PageGeom &g, int Tq, int64_t tokens)
@@ -119,7 +120,7 @@ static PageAttnPlan plan_page_attn(const kvev_shape *sh, const PageGeom &g, int 
     PageAttnPlan p = plan_page_form(sh, g, Tq, tokens, false);
     if (sh->dtype != KVEV_BF16 || (int64_t)(sh->H / g.Hkv) * Tq < kFrameQueries) return p;
     PageAttnPlan f = plan_page_form(sh, g, Tq, tokens, true);
-    f.ws_any = p.ws_any = std::max(p.ws_any, f.ws_any);      // (the form depends on the length as well)
+    f.ws_any = p.ws_any = std::max(p.ws_any, f.ws_any);      // (the form depends on the length and the queries as well)
     return p.units * tokens >= g_frame_work.load() ? f : p;
 }
 static bool page_queries_fit(const kvev_shape *sh, int Tq) { return (int64_t)sh->L * sh->B * sh->H * Tq <= (int64_t)1 << 26; }

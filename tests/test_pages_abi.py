@@ -129,6 +129,18 @@ def test_workspaces():
     assert kb.page_workspace_bytes(kb.OP_PAGE_ATTENTION, sh, kb.make_pages(17, 1, 1), 1) == 0
 
 
+@pytest.mark.parametrize("L,B,H,H_kv", [(1, 1, 1, 0), (1, 2, 32, 8), (2, 64, 32, 8), (32, 8, 8, 8)])
+def test_attention_workspace_serves_fewer_queries(L, B, H, H_kv):
+    for d, dtype in ((64, kb.F32), (128, kb.BF16)):
+        sh, last = _shape(L=L, B=B, H=H, H_kv=H_kv, d=d, dtype=dtype, T=0), 0
+        for Tq in (1, 2, 5, 16, 17, 40, 48, 64, 100, 128, 129, 256, 257, 700, 1024):
+            need = kb.page_workspace_bytes(kb.OP_PAGE_ATTENTION, sh, kb.make_pages(64, 100, 150), Tq)
+            assert need >= last > -1 and need > 0, (d, dtype, Tq)
+            last = need
+        # rows of one run: nothing to join
+        assert kb.page_workspace_bytes(kb.OP_PAGE_ATTENTION, sh, kb.make_pages(64, 100, 3), 1) == 0
+
+
 def test_pool_size():
     assert kb.page_pool_bytes(_shape(), kb.make_pages(32, 10, 7)) == 2 * 10 * 4 * 32 * (128 + 8)
     assert kb.page_pool_bytes(_shape(d=64, H_kv=0), kb.make_pages(16, 3, 7)) == 2 * 3 * 8 * 16 * (64 + 4)

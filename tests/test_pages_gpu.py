@@ -349,6 +349,33 @@ def test_attention_forms():
     assert kb.kvev_debug_page_form(shape_of(1, 16, 32, 8, T=8192, dtype=torch.float32), pages, 256)[0] == 16
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_calls_of_every_size_take_one_workspace(dtype, frames):
+    """Prompts, decode steps and growing rows in turn: whatever a call leaves in the scratch, the next one finds its tickets at zero."""
+    lengths = [5900, 1300, 64]
+    sh = shape_of(1, 3, 8, 4, 64, dtype, 5900)
+    c = cache_of(sh, 64, lengths, Tq=150)
+    fill(c, lengths, dtype)
+    sizes, forms = [(150, 5900), (1, 5900), (20, 5900), (1, 2000), (7, 0), (23, 1400), (100, 300), (2, 5900)], set()
+    Q = {Tq: normal(Tq, 1, 3, 8, Tq, 64, dtype=dtype) for Tq, _ in sizes}
+    want = {}
+    for Tq, T in sizes:                                  # each with scratch of its own
+        sh.T = T
+        forms.add(kb.kvev_debug_page_form(sh, c.pages, Tq))
+        want[Tq, T] = torch.full_like(Q[Tq], 9.0)
+        ws = kb.alloc_workspace(kb.page_workspace_bytes(kb.OP_PAGE_ATTENTION, sh, c.pages, Tq), "cuda")
+        kb.kvev_page_attention(sh, c.pages, Q[Tq], Tq, c.pool, c.table, c.length, want[Tq, T], ws)
+    assert len({queries for queries, _, runs in forms if runs > 1}) == (2 if dtype == torch.bfloat16 else 1), forms
+    for turn in range(3):
+        for Tq, T in random.Random(turn).sample(sizes, len(sizes)) + sizes:
+            sh.T = T
+            O = torch.full_like(Q[Tq], -9.0)
+            c.attend(Q[Tq], Tq, O)
+            assert torch.equal(O, want[Tq, T]), (turn, Tq, T)
+    sh.T = 0
+    check_attention(c, Q[1], want[1, 5900], lengths, heads=[(0, b, b) for b in range(3)])
+
+
 @pytest.mark.parametrize("Tq", [1, 40])
 def test_attention_over_a_window(Tq, frames):
     """Tokens before `first` and pages given up; entries that are no page inside the window; lengths that are wrong."""
