@@ -5,18 +5,19 @@
 // most of them for far tokens.  What is left of a turn goes to sine and cosine in fp32 (an error of 2^-25 turns).  They depend on
 // the token and not on the head, so a thread makes those of its pairs once and takes them through the heads of its slice;
 // queries and keys of one call are one list of heads.  Bytes bound it, sine and cosine where a token has few heads: 64 rows x 256
-// tokens x (32 + 8) heads, bf16, d = 128: 65 us, 5.2 TB/s in and out, what a copy of that size reaches.  Where the pairs are no
-// multiple of a piece, halves pay for the ends of pieces element by element (4 x 1000 x 64 heads, 61 pairs: 51 us, as
-// neighbouring pairs 23 us).  Tried and dropped: non-temporal accesses (no difference); ends in halves and quarters of a piece (scratch: 76 us).
+// tokens x (32 + 8) heads, bf16, d = 128: 65 - 71 us, 4.7 - 5.2 TB/s in and out, what a copy of that size reaches.  Where the pairs are
+// no multiple of a piece, halves pay for the ends of pieces (4 x 1000 x 64 heads, 61 pairs: 31 us, as neighbouring pairs 23; with
+// ends element by element 51).  Tried and dropped: non-temporal accesses (no difference).
 #include "kernels.hpp"
 #include "pages.hpp"
 
 namespace kvev {
 
-// Pieces of up to 16 bytes (W elements), wherever they begin: memory takes such accesses at any element.
-template <typename T, int W> __device__ __forceinline__ void get_piece(const T *p, int n, float (&o)[W])
+// Pieces of up to 16 bytes (W elements), wherever they begin: memory takes such accesses at any element.  A piece of n < W elements
+// is read whole where the tensor goes on behind it (`end`), and written in 8, 4 and 2 bytes.
+template <typename T, int W> __device__ __forceinline__ void get_piece(const T *p, int n, const T *end, float (&o)[W])
 {
-    if (n >= W) {
+    if (n >= W || end - p >= W) {
         u32x4_t w;
         __builtin_memcpy(&w, p, 16);
 #pragma unroll
@@ -28,21 +29,36 @@ template <typename T, int W> __device__ __forceinline__ void get_piece(const T *
 }
 template <typename T, int W> __device__ __forceinline__ void put_piece(T *p, int n, const float (&o)[W])
 {
-    if (n >= W) {
-        u32x4_t w;
+    uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = sizeof(T) == 4 ? __float_as_uint(o[i]) : pack_bf16x2(o[(2 * i) % W], o[(2 * i + 1) % W]);
-        __builtin_memcpy(p, &w, 16);
-        hold_store_data(w);
+    for (int i = 0; i < 4; ++i) w[i] = sizeof(T) == 4 ? __float_as_uint(o[i]) : pack_bf16x2(o[(2 * i) % W], o[(2 * i + 1) % W]);
+    if (n >= W) {
+        u32x4_t v = {w[0], w[1], w[2], w[3]};
+        __builtin_memcpy(p, &v, 16);
+        hold_store_data(v);
         return;
     }
-#pragma unroll
-    for (int i = 0; i < W; ++i)
-        if (i < n) Storage<T>::store(p + i, o[i]);
+    constexpr int PW = 4 / (int)sizeof(T);       // elements of a word
+    const int words = n / PW;
+    if (words & 2) {
+        const uint2 v = make_uint2(w[0], w[1]);
+        __builtin_memcpy(p, &v, 8);
+    }
+    if (words & 1) {
+        const uint32_t v = words & 2 ? w[2] : w[0];
+        __builtin_memcpy(p + (words & 2) * PW, &v, 4);
+    }
+    if (PW == 2 && (n & 1)) {
+        const uint32_t v = words & 2 ? (words & 1 ? w[3] : w[2]) : (words & 1 ? w[1] : w[0]);
+        const uint16_t lo = (uint16_t)v;
+        __builtin_memcpy(p + words * PW, &lo, 2);
+    }
 }
 
-// A slot of a head is a piece.  Halves (ADJ false): up to W pairs, at j and at pairs + j, then the elements behind the turned ones, W
-// at a time.  Adjacent: W elements of the head, W / 2 pairs, those from `pairs` on as they are.
+// A slot of a head is a piece.  Halves (ADJ false): up to W pairs, at j and at pairs + j, then the elements behind the turned ones, up
+// to the next multiple of W and on in whole pieces.  Adjacent: W elements of the head, W / 2 pairs, those from `pairs` on as they are.
+template <int W> __host__ __device__ inline int tail_pieces_at(int pairs) { return 2 * pairs / W * W; }
+
 template <typename T, bool ADJ>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int slots, int tb, int ttiles, int slices)
 {
@@ -55,8 +71,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int slots, in
 
     const int j0 = slot * NP, turned = (a.pairs + NP - 1) / NP;  // first pair; slots that have pairs
     const bool turn = slot < turned;
-    const int e0 = ADJ ? slot * W : turn ? j0 : 2 * a.pairs + (slot - turned) * W;
-    const int n = ADJ ? W : min(W, turn ? a.pairs - j0 : a.d - e0);
+    const int whole = tail_pieces_at<W>(a.pairs), tail = whole + (slot - turned) * W;
+    const int e0 = ADJ ? slot * W : turn ? j0 : max(tail, 2 * a.pairs);
+    const int n = ADJ ? W : turn ? min(W, a.pairs - j0) : tail + W - e0;
     float cs[NP], sn[NP];
     if (turn) {
         int at[4];
@@ -80,8 +97,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int slots, in
         const size_t off = ((((size_t)l * a.B + b) * H + h) * a.Tq + t) * a.d + e0;
         const T *x = static_cast<const T *>(q ? a.Q : a.K) + off;
         T *y = static_cast<T *>(q ? a.Qo : a.Ko) + off;
+        const T *end = static_cast<const T *>(q ? a.Q : a.K) + (size_t)a.L * a.B * H * a.Tq * a.d;
         float u[W], v[W];
-        get_piece<T, W>(x, n, u);
+        get_piece<T, W>(x, n, end, u);
         if (!turn) {
             put_piece<T, W>(y, n, u);
             continue;
@@ -96,7 +114,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int slots, in
             }
             put_piece<T, W>(y, n, p);
         } else {
-            get_piece<T, W>(x + a.pairs, n, v);
+            get_piece<T, W>(x + a.pairs, n, end, v);
             float m[W];
 #pragma unroll
             for (int i = 0; i < W; ++i) {
@@ -113,7 +131,7 @@ template <typename T>
 static hipError_t launch_rotary_as(const RotaryArgs &a, hipStream_t st)
 {
     constexpr int W = 16 / (int)sizeof(T);
-    const int slots = a.adjacent ? a.d / W : (a.pairs + W - 1) / W + (a.d - 2 * a.pairs + W - 1) / W;        // (at most 33)
+    const int slots = a.adjacent ? a.d / W : (a.pairs + W - 1) / W + (a.d - tail_pieces_at<W>(a.pairs)) / W;        // (at most 33)
     // a workgroup takes up to 32 tokens; what is left of its threads takes heads side by side
     int tb = 1;
     while (tb < 32 && tb < a.Tq && tb * 2 * slots <= 256) tb *= 2;
