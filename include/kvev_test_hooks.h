@@ -72,8 +72,14 @@ int kvev_debug_attn_stream_bytes(size_t bytes);
  * kernels.  Errors: INVALID_ARG for a negative value. */
 int kvev_debug_page_frame_work(int64_t work);
 
-/* How a kvev_page_attention call would run: queries of a unit (16; a frame's 128
- * or 256), waves of a workgroup and the most workgroups that share a unit's rows.
+/* kvev_page_attention takes calls of bf16 storage with 17 queries or more to a
+ * key-value head in units of 32 instead of 16 where these are at least `units`
+ * (0 restores the rule).  1 lets small shapes walk that form.  Errors: INVALID_ARG
+ * for a negative value. */
+int kvev_debug_page_pair_units(int64_t units);
+
+/* How a kvev_page_attention call would run: queries of a unit (16 or 32; a
+ * frame's 128 or 256), waves of a workgroup and the most workgroups that share a unit's rows.
  * Errors: INVALID_ARG. */
 int kvev_debug_page_form(const kvev_shape *shape, const kvev_pages *pages, int Tq, int *queries, int *waves, int *runs);
 

@@ -41,7 +41,8 @@ EXPORTS = ("kvev_chunk_pool", "kvev_lstm_gate", "kvev_lstm_prepare", "kvev_lstm_
            "kvev_pages_reserve", "kvev_pages_fork", "kvev_pages_trim", "kvev_pages_copy", "kvev_pages_compact", "kvev_rotary")
 TEST_HOOKS = ("kvev_debug_pair_wait", "kvev_debug_lstm_fused_min_groups", "kvev_debug_lstm_quad_groups", "kvev_debug_stream_probe",
               "kvev_debug_attn_stream_bytes", "kvev_debug_lstm_plan", "kvev_debug_lstm_form",
-              "kvev_debug_pool_form", "kvev_debug_decode_queries", "kvev_debug_page_frame_work", "kvev_debug_page_form")      # include/kvev_test_hooks.h
+              "kvev_debug_pool_form", "kvev_debug_decode_queries", "kvev_debug_page_frame_work", "kvev_debug_page_pair_units",
+              "kvev_debug_page_form")      # include/kvev_test_hooks.h
 
 
 class Shape(ctypes.Structure):
@@ -127,6 +128,8 @@ def lib() -> ctypes.CDLL:
         L.kvev_debug_decode_queries.restype = ci
         L.kvev_debug_page_frame_work.argtypes = [ctypes.c_int64]
         L.kvev_debug_page_frame_work.restype = ci
+        L.kvev_debug_page_pair_units.argtypes = [ctypes.c_int64]
+        L.kvev_debug_page_pair_units.restype = ci
         L.kvev_debug_page_form.argtypes = [shp, ctypes.POINTER(Pages), ci, ctypes.POINTER(ci), ctypes.POINTER(ci), ctypes.POINTER(ci)]
         L.kvev_debug_page_form.restype = ci
         L.kvev_debug_lstm_form.argtypes = [shp, ci, ctypes.POINTER(ci)]
@@ -250,6 +253,10 @@ def kvev_debug_decode_queries(shape: Shape, Tq: int, k_cap: int) -> int:
 
 def kvev_debug_page_frame_work(work: int = 0) -> None:
     _check(lib().kvev_debug_page_frame_work(work), "kvev_debug_page_frame_work")
+
+
+def kvev_debug_page_pair_units(units: int = 0) -> None:
+    _check(lib().kvev_debug_page_pair_units(units), "kvev_debug_page_pair_units")
 
 
 def kvev_debug_page_form(shape: Shape, pages: "Pages", Tq: int) -> Tuple[int, int, int]:

@@ -42,7 +42,7 @@ static size_t elem(const kvev_shape *sh) { return sh->dtype == KVEV_F32 ? 4 : 2;
 static size_t pool_bytes(const PageGeom &g) { return (size_t)g.L * g.n_pages * page_bytes(g); }
 
 // ---- attention over pages: planning ----
-// A unit is 16 queries of a key-value head; its rows, in chunks of 64 for one wave each, are cut into runs of `run` chunks, a
+// A unit is 16 or 32 queries of a key-value head; its rows, in chunks of 64 for one wave each, are cut into runs of `run` chunks, a
 // workgroup of 1, 4 or 8 waves each.  A batch row takes as many of a unit's nsplit workgroups as its own length pays for
 // (decided on the device, where the lengths are).  shape->T, or the capacity if it is 0, says for which length the launch is made;
 // results depend on it in the order of sums and the choice of form only.
@@ -57,19 +57,28 @@ static size_t pool_bytes(const PageGeom &g) { return (size_t)g.L * g.n_pages * p
 //     runs for four workgroups per compute unit, of 16 chunks at least: they hide each other's ends, and long rows of a ragged
 //     batch are spread (32 x 16000 tokens 19.9 us, one workgroup per compute unit 22.0; 512 units of 64 ragged rows up to 8192
 //     tokens 63, unsplit 72; 128 units of 16 ragged rows up to 12000 29 and 47).
-// Frames (page_frame.hip; bf16): units of 128 or 256 queries, two workgroups or one per compute unit.  They take calls with 48 queries or more to a key-value head and enough work
-// (units of 16 queries x tokens; 4 query heads to a key-value head, units of 16 and frame, us): 128 heads x 64 queries x 4000
-// tokens 54.2 and 52.6; 128 x 128 x 600 24.2 and 26.0; 128 x 256 x 600 34.7 and 33.9; 512 x 64 x 600 40.8 and 32.6; 8 x 1024 x
-// 4000 47.8 and 41.8; but 8 x 1024 x 600 12.9 and 23.5, 8 x 256 x 4000 19.9 and 34.4, and 512 x 32 x 4000 106 and 124.
+// Units of 32 queries (bf16) convert a row once for all of them, but leave registers for two waves on a SIMD and half the units: they are
+// taken where they are two per compute unit, or half as many with enough rows (units of 16 and 32, us; 32 queries to a key-value
+// head: 512 heads x 200 tokens 13.3 and 11.2, x 4000 110 and 73; 256 x 300 9.2 and 10.4, x 1000 17.6 and 16.6, x 4000 54 and 42; 128 x
+// 4000 33.8 and 28.2, of 16 ragged rows up to 8192 36.6 and 39.1; 32 x 4000 15.6 and 19.4).  Their runs give every compute unit two
+// workgroups, all that it holds at once (four: 81 and 47 at 512 and 256 heads x 4000).
+// Frames (page_frame.hip; bf16): units of 128 or 256 queries, two workgroups or one per compute unit.  They take calls with 48 queries
+// or more to a key-value head (65 where units of 32 are taken: 128 heads x 64 queries x 8192 tokens 70 and 84, 512 x 64 x 600
+// 32.3 and 29.4) and enough work (units of 16 queries x tokens; 4 query heads to a key-value head, units of 16 and frame, us):
+// 128 x 128 x 600 23.7 and 22.1; 128 x 256 x 600 32.6 and 29.0; 8 x 1024 x 4000 45.7 and 38.6; but 8 x 1024 x 600 12.1 and 22.2, 8 x 256
+// x 4000 19.9 and 34.4.
 constexpr int kPageChunk = 64, kPageMaxSplit = 64, kFrameQueries = 48, kFrameRounds = 3;
 constexpr int64_t kFrameWork = 1200000;
+constexpr int64_t kPairWork = 2000, kPairMost = 64;
 static std::atomic<int64_t> g_frame_work{kFrameWork};      // (kvev_debug_page_frame_work lowers it)
+static std::atomic<int64_t> g_pair_units{0};               // (kvev_debug_page_pair_units: 0: by the rule)
 struct PageAttnPlan { int queries, waves, qtiles, nsplit, run; int64_t units; size_t ticket_bytes, ws_bytes, ws_any; };
-static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int Tq, int64_t tokens, bool frame)
+static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int Tq, int64_t tokens, int queries)
 {
     PageAttnPlan p;
     const int64_t R = (int64_t)(sh->H / g.Hkv) * Tq, cus = device_compute_units(), cap = (int64_t)g.max_pages << g.page_shift;
-    p.queries = !frame ? 16 : R <= 128 ? 128 : 256;
+    const bool frame = queries > 32;
+    p.queries = queries;
     p.qtiles = (int)((R + p.queries - 1) / p.queries);
     p.units = (int64_t)g.L * g.B * g.Hkv * p.qtiles;
     const int64_t chunks = (tokens + kPageChunk - 1) / kPageChunk, slots = p.queries == 128 ? 2 * cus : cus;
@@ -88,7 +97,7 @@ static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int 
             if (n == 1 || t < least) { least = t; best = n; }
         }
         run = (chunks + best - 1) / best;
-    } else if (sh->dtype == KVEV_F32 ? p.units <= cus : p.units * ((chunks + 7) / 8) <= cus) {
+    } else if (queries == 16 && (sh->dtype == KVEV_F32 ? p.units <= cus : p.units * ((chunks + 7) / 8) <= cus)) {
         p.waves = 8;
         const int64_t n = std::max<int64_t>(cus / p.units, 1);
         run = std::max<int64_t>((chunks + n - 1) / n, 8);
@@ -98,7 +107,7 @@ static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int 
     } else {
         p.waves = 4;
         run = std::max<int64_t>(fill(cus), 4);
-        if (run > 16) run = std::max<int64_t>(fill(4 * cus), 16);
+        if (run > 16) run = std::max<int64_t>(fill((queries == 32 ? 2 : 4) * cus), 16);
     }
     run = std::min(std::max(run, (chunks + kPageMaxSplit - 1) / kPageMaxSplit), std::max<int64_t>(chunks, 1));
     p.run = (int)run;
@@ -107,7 +116,7 @@ static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int 
     // One ticket per unit of 16 queries that is split; four workgroups per compute unit bound their number, and room for as many
     // stands first whatever the call: the partials of one call then never lie where another one has its tickets.
     p.ticket_bytes = ((size_t)4 * cus * sizeof(int32_t) + 255) / 256 * 256;
-    const size_t partial = (!frame ? (size_t)16 * (g.d + 2) : (size_t)p.queries * (g.d + 4)) * sizeof(float);
+    const size_t partial = (size_t)p.queries * (g.d + (frame ? 4 : 2)) * sizeof(float);
     p.ws_bytes = p.nsplit > 1 ? p.ticket_bytes + (size_t)p.units * p.nsplit * partial : 0;
     // enough for every length of row and for fewer queries: split units take the workgroups wanted (rounded up to the unit), and no
     // run is shorter than 4 chunks
@@ -117,11 +126,22 @@ static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int 
 }
 static PageAttnPlan plan_page_attn(const kvev_shape *sh, const PageGeom &g, int Tq, int64_t tokens)
 {
-    PageAttnPlan p = plan_page_form(sh, g, Tq, tokens, false);
-    if (sh->dtype != KVEV_BF16 || (int64_t)(sh->H / g.Hkv) * Tq < kFrameQueries) return p;
-    PageAttnPlan f = plan_page_form(sh, g, Tq, tokens, true);
-    f.ws_any = p.ws_any = std::max(p.ws_any, f.ws_any);      // (the form depends on the length and the queries as well)
-    return p.units * tokens >= g_frame_work.load() ? f : p;
+    const int64_t R = (int64_t)(sh->H / g.Hkv) * Tq, cus = device_compute_units(), pairs = g_pair_units.load();
+    PageAttnPlan best = plan_page_form(sh, g, Tq, tokens, 16);
+    if (sh->dtype != KVEV_BF16 || R <= 16) return best;
+    const int64_t work = best.units * tokens;
+    size_t any = best.ws_any;                    // (the form depends on the length and the queries as well)
+    const PageAttnPlan p = plan_page_form(sh, g, Tq, tokens, 32);
+    any = std::max(any, p.ws_any);
+    const bool pair = pairs > 0 ? p.units >= pairs : p.units >= 2 * cus || (2 * p.units >= cus && p.units * tokens >= kPairWork * cus);
+    if (pair) best = p;
+    if (R >= kFrameQueries) {
+        const PageAttnPlan f = plan_page_form(sh, g, Tq, tokens, R <= 128 ? 128 : 256);
+        any = std::max(any, f.ws_any);
+        if (work >= g_frame_work.load() && !(pair && R <= kPairMost)) best = f;
+    }
+    best.ws_any = any;
+    return best;
 }
 static bool page_queries_fit(const kvev_shape *sh, int Tq) { return (int64_t)sh->L * sh->B * sh->H * Tq <= (int64_t)1 << 26; }
 static int64_t plan_tokens(const kvev_shape *sh, const PageGeom &g)
@@ -158,6 +178,13 @@ int kvev_debug_page_frame_work(int64_t work)
 {
     if (work < 0) return KVEV_ERR_INVALID_ARG;
     g_frame_work = work == 0 ? kFrameWork : work;
+    return KVEV_OK;
+}
+
+int kvev_debug_page_pair_units(int64_t units)
+{
+    if (units < 0) return KVEV_ERR_INVALID_ARG;
+    g_pair_units = units;
     return KVEV_OK;
 }
 
@@ -280,7 +307,7 @@ int kvev_page_attention(const kvev_shape *sh, const kvev_pages *pg, const void *
     }
     a.stream = (size_t)sh->L * sh->B * a.g.Hkv * (size_t)plan_tokens(sh, a.g) * 17 * sh->d / 16 > attn_stream_bytes();
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)sh->d));
-    const hipError_t e = p.queries == 16 ? launch_page_attention(a, sh->dtype, p.waves, static_cast<hipStream_t>(stream))
+    const hipError_t e = p.queries <= 32 ? launch_page_attention(a, sh->dtype, p.queries, p.waves, static_cast<hipStream_t>(stream))
                                          : launch_page_frame(a, p.queries, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? KVEV_OK : hip_fail(e);
 }

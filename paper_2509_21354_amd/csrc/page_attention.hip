@@ -11,8 +11,15 @@
 //                 8 kk .. 8 kk + 7 of every lane's quarter, and the queries are loaded the same way.)
 //   O^T = V^T P^T A = V^T through LDS: values converted as above go to a wave's own 32 rows and come back by the transposing
 //                 load; B = the weights where the first product left them.
-// A wave takes chunks of 64 rows; the four waves of a workgroup take chunks in turn and meet in LDS at the end, the workgroups
-// that share a unit's rows meet in scratch (partials, a ticket, the last one to arrive merges in split order).
+// A wave takes chunks of 64 rows; the waves of a workgroup (1, 4 or 8) take chunks in turn and meet in LDS at the end, the workgroups
+// that share a unit's rows meet in scratch (partials, a ticket, the last one to arrive merges in split order).  A unit has one or
+// two such tiles of 16 queries (QT): with two, converting and staging a row is paid once for both (512 heads x 32 queries x 4000
+// tokens 110 and 73 us).
+// What bounds it (d = 128, bf16): 32 layers x 8 rows x 8 heads x 8192 tokens, 2.29 GB, 365 - 374 us = 6.1 - 6.3 TB/s with the vector unit 54 %
+// and the matrix cores 27 % busy, a reader without arithmetic reaches 7.2; 64 x 8 heads of ragged rows up to 8192 61 us = 4.8 TB/s (the
+// ends of rows, the join); 32 heads x 4091 tokens 11 us (launch and a chain of five round trips: length and table, codes, partials,
+// ticket, partials again).  Four waves on a SIMD spill (629 us).  Tried and dropped, no gain: prefetching without branches, a peeled last
+// chunk, store rows asked for ahead; equal shares of all chunks for as many workgroups as fit (410).
 // fp32: the queries enter as three bf16 terms of 8 bits, the weights likewise, rows of the store too (products of terms below
 // 2^-24 left out).  bf16: the weights enter as two terms.
 //
@@ -114,8 +121,8 @@ template <int D> __device__ __forceinline__ int turn_of(int t)
 // bytes of LDS of a wave: its staging rows, then its outputs
 template <int D> constexpr int wave_lds() { return 32 * D * 2 > 16 * (D + 4) * 4 ? 32 * D * 2 : 16 * (D + 4) * 4; }
 
-template <typename T, int D, int NW, bool STREAM>
-__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void page_attention_kernel(PageAttnArgs a)
+template <typename T, int D, int NW, bool STREAM, int QT>
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 && QT == 1 ? 3 : 2) void page_attention_kernel(PageAttnArgs a)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int NQ = Terms<T>::Q, NP = Terms<T>::P, KS = D / 32, DT = D / 16, NB = D / 32;
@@ -134,12 +141,14 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void pag
     const int qt = unit % a.qtiles, s = unit / a.qtiles, h = s % g.Hkv, lb = s / g.Hkv, b = lb % g.B, l = lb / g.B;
     const int R = a.G * a.Tq, cap = g.max_pages << g.page_shift;
 
-    // this lane's query
-    const int r = qt * 16 + n, rc = min(r, R - 1), gq = rc / a.Tq, tq = rc - gq * a.Tq;
-    const size_t orow = (((size_t)lb * g.Hkv + h) * a.G + gq) * a.Tq + tq;
-    bf16x8_t qf[KS][NQ];
+    // this lane's queries (rows s R .. s R + R - 1 of Q and O are those of the key-value head)
+    bf16x8_t qf[QT][KS][NQ];
 #pragma unroll
-    for (int kk = 0; kk < KS; ++kk) Terms<T>::load(static_cast<const T *>(a.Q) + orow * D + gr * (D / 4) + kk * 8, qf[kk]);
+    for (int u = 0; u < QT; ++u) {
+        const size_t row = (size_t)s * R + min((qt * QT + u) * 16 + n, R - 1);
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) Terms<T>::load(static_cast<const T *>(a.Q) + row * D + gr * (D / 4) + kk * 8, qf[u][kk]);
+    }
 
     // Lane 4 j + i holds the table's entry for group i of this wave's chunk j (of 16; its chunks lie NW apart): asked for before the length is there, as if
     // the rows were the pages' from the beginning on and the run as long as planned, which they are most of the time.
@@ -157,20 +166,29 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void pag
     if (split >= active) return;
     const int c0 = split * per, c1 = min(chunks, c0 + per);
 
-    int lim = len - 1, lim_all = len - 1;        // the last token that this lane's query sees, and that all of the unit's see
+    int lim[QT], lim_all = len - 1;              // the last token that this lane's queries see, and that all of the unit's see
+#pragma unroll
+    for (int u = 0; u < QT; ++u) lim[u] = len - 1;
     if (a.q_start) {
         const int64_t at = a.q_start[b];
-        lim = (int)min<int64_t>(lim, at + tq);
+        const int q0 = qt * QT * 16, q1 = min(q0 + QT * 16, R) - 1;
+#pragma unroll
+        for (int u = 0; u < QT; ++u) lim[u] = (int)min<int64_t>(lim[u], at + min(q0 + u * 16 + n, R - 1) % a.Tq);
         // (a unit whose queries are the ends of two heads and the beginning of a third has token 0 among them)
-        const int t0 = qt * 16 / a.Tq == min(qt * 16 + 15, R - 1) / a.Tq ? qt * 16 % a.Tq : 0;
-        lim_all = (int)min<int64_t>(lim_all, at + t0);
+        lim_all = (int)min<int64_t>(lim_all, at + (q0 / a.Tq == q1 / a.Tq ? q0 % a.Tq : 0));
     }
 
-    float m = -INFINITY, lsum = 0.f;             // scaled running maximum and this lane's part of the sum, of query n
-    f32x4_t o[DT];
+    float m[QT], lsum[QT];                       // scaled running maximum and this lane's part of the sum, of query n of each tile
+    f32x4_t o[QT][DT];
+    uint32_t nan_blocks[QT];                     // blocks of d whose values are NaN in a token that the query sees
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    uint32_t nan_blocks = 0;                     // blocks of d whose values are NaN in a token that query n sees
+    for (int u = 0; u < QT; ++u) {
+        m[u] = -INFINITY;
+        lsum[u] = 0.f;
+        nan_blocks[u] = 0;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[u][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
 
     // staging: lane (n, gr) writes pieces gr * KS + kk of tokens n and 16 + n; it reads, of tokens 4 gr + n / 4 and 16 further on, piece
     // 2 dt + (n & 3) / 2, half n & 1
@@ -186,21 +204,21 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void pag
     const unsigned char *pool = a.pool + ((size_t)l * g.n_pages * g.Hkv + h) * block;
 
     // the weights of a chunk from its scores (hidden ones: -inf), and the running state
-    auto soft = [&](f32x4_t (&st)[4], bf16x8_t (&pb)[2][NP]) __attribute__((always_inline)) {
+    auto soft = [&](int u, f32x4_t (&st)[4], bf16x8_t (&pb)[2][NP]) __attribute__((always_inline)) {
         float mx = max3(st[0][0], st[0][1], st[0][2]);
         mx = max3(mx, st[0][3], st[1][0]);
 #pragma unroll
         for (int i = 5; i < 15; i += 2) mx = max3(mx, st[i / 4][i % 4], st[(i + 1) / 4][(i + 1) % 4]);
         mx = rows_max(fmaxf(mx, st[3][3])) * c;
-        const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
-        if (__any(m_new > m)) {
-            const float alpha = __builtin_amdgcn_exp2f(m - ref);
-            lsum *= alpha;
+        const float m_new = fmaxf(m[u], mx), ref = m_new == -INFINITY ? 0.f : m_new;
+        if (__any(m_new > m[u])) {
+            const float alpha = __builtin_amdgcn_exp2f(m[u] - ref);
+            lsum[u] *= alpha;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[dt][e] *= alpha;
-            m = m_new;
+                for (int e = 0; e < 4; ++e) o[u][dt][e] *= alpha;
+            m[u] = m_new;
         }
         // (The multiply-add leaves the rounding of the maximum's product in every weight, a factor that the normaliser shares.
         // Where it is no longer near 1, the products are rounded first.)
@@ -218,7 +236,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void pag
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 p[e] = __builtin_amdgcn_exp2f(fmaf(st[2 * h2 + (e >> 2)][e & 3], cc, -ref));
-                lsum += p[e];
+                lsum[u] += p[e];
             }
             cut_weights<NP>(p, pb[h2]);
         }
@@ -230,7 +248,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void pag
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     };
     // O^T += V^T P^T over them: one term of the values, with the weights' terms that matter (all but the last `skip`)
-    auto values = [&](const bf16x8_t (&pb)[NP], int skip) __attribute__((always_inline)) {
+    auto values = [&](const bf16x8_t (&pb)[QT][2][NP], int h2, int skip) __attribute__((always_inline)) {
         hold();
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
@@ -239,8 +257,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void pag
             const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)(src + 16 * 2 * D));
             const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-            for (int k = NP - 1; k >= 0; --k)
-                if (k + skip < NP) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[k], o[dt], 0, 0, 0);
+            for (int u = 0; u < QT; ++u)
+#pragma unroll
+                for (int k = NP - 1; k >= 0; --k)
+                    if (k + skip < NP) o[u][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[u][h2][k], o[u][dt], 0, 0, 0);
         }
         hold();
     };
@@ -248,27 +268,33 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void pag
     // ---- rows of the store ----
     int ch = c0 + wave;
     for (; ch < min(sc, c1); ch += NW) {
-        f32x4_t st[4];
-        bf16x8_t pb[2][NP];
+        f32x4_t st[QT][4];
+        bf16x8_t pb[QT][2][NP];
         const T *Kc = static_cast<const T *>(a.Kc) + (size_t)s * a.k_cap * D, *Vc = static_cast<const T *>(a.Vc) + (size_t)s * a.k_cap * D;
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
             const int j0 = ch * 64 + kt * 16, j = min(j0 + n, kept - 1);
-            st[kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < QT; ++u) st[u][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int kk = 0; kk < KS; ++kk) {
                 bf16x8_t kf[NQ];
                 Terms<T>::load(Kc + (size_t)j * D + gr * (D / 4) + kk * 8, kf);
 #pragma unroll
-                for (int x = NQ - 1; x >= 0; --x)
+                for (int u = 0; u < QT; ++u)
 #pragma unroll
-                    for (int y = NQ - 1 - x; y >= 0; --y) st[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x], qf[kk][y], st[kt], 0, 0, 0);
+                    for (int x = NQ - 1; x >= 0; --x)
+#pragma unroll
+                        for (int y = NQ - 1 - x; y >= 0; --y) st[u][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x], qf[u][kk][y], st[u][kt], 0, 0, 0);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (j0 + 4 * gr + e >= kept) st[kt][e] = -INFINITY;
+            for (int u = 0; u < QT; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j0 + 4 * gr + e >= kept) st[u][kt][e] = -INFINITY;
         }
-        soft(st, pb);
+#pragma unroll
+        for (int u = 0; u < QT; ++u) soft(u, st[u], pb[u]);
 #pragma unroll
         for (int h2 = 0; h2 < 2; ++h2)
 #pragma unroll
@@ -284,7 +310,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void pag
                         *reinterpret_cast<bf16x8_t *>(put[kk] + i * 16 * 2 * D) = vf[x];
                     }
                 }
-                values(pb[h2], x);
+                values(pb, h2, x);
             }
     }
 
@@ -335,16 +361,19 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void pag
             for (int i = 0; i < 4; ++i)
                 if ((gone >> i & 1) || t0 + 16 * i + n < first || t0 + 16 * i + n >= len) { vc[i] = codes_t{}; sv[i] = 127u << 8; }
         }
-        f32x4_t st[4];
-        bf16x8_t pb[2][NP];
+        f32x4_t st[QT][4];
+        bf16x8_t pb[QT][2][NP];
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
-            st[kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < QT; ++u) st[u][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int kk = 0; kk < KS; ++kk) {
                 const bf16x8_t kf = unpack8(kc[kt][kk], __uint_as_float(sk[kt] << 23));
 #pragma unroll
-                for (int y = NQ - 1; y >= 0; --y) st[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[kk][y], st[kt], 0, 0, 0);
+                for (int u = 0; u < QT; ++u)
+#pragma unroll
+                    for (int y = NQ - 1; y >= 0; --y) st[u][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[u][kk][y], st[u][kt], 0, 0, 0);
             }
         }
         if (j + 1 < mine) {
@@ -356,14 +385,17 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void pag
         }
         if (!full) {
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
+            for (int u = 0; u < QT; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int t = t0 + 16 * kt + 4 * gr + e;
-                    if ((gone >> kt & 1) || t < first || t > lim) st[kt][e] = -INFINITY;
-                }
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int t = t0 + 16 * kt + 4 * gr + e;
+                        if ((gone >> kt & 1) || t < first || t > lim[u]) st[u][kt][e] = -INFINITY;
+                    }
         }
-        soft(st, pb);
+#pragma unroll
+        for (int u = 0; u < QT; ++u) soft(u, st[u], pb[u]);
         if (__any(max(max(sv[0], sv[1]), max(sv[2], sv[3])) >= kNanScale << 8)) {       // (rare)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -371,7 +403,9 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void pag
                 while (bad) {
                     const int x = __builtin_ctzll(bad);
                     bad &= bad - 1;
-                    if (t0 + 16 * i + (x & 15) <= lim) nan_blocks |= 1u << ((x >> 4) * NB / 4);
+#pragma unroll
+                    for (int u = 0; u < QT; ++u)
+                        if (t0 + 16 * i + (x & 15) <= lim[u]) nan_blocks[u] |= 1u << ((x >> 4) * NB / 4);
                 }
                 if (sv[i] >= kNanScale << 8) { vc[i] = codes_t{}; sv[i] = 127u << 8; }
             }
@@ -384,57 +418,60 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void pag
                 for (int kk = 0; kk < KS; ++kk)
                     *reinterpret_cast<bf16x8_t *>(put[kk] + i * 16 * 2 * D) = unpack8(vc[2 * h2 + i][kk], __uint_as_float(sv[2 * h2 + i] << 15));
             if (h2 == 1 && j + 1 < mine) fetch_values();
-            values(pb[h2], 0);
+            values(pb, h2, 0);
         }
     }
-    if (nan_blocks) {
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-            if (nan_blocks >> (dt / 2) & 1) o[dt] = f32x4_t{NAN, NAN, NAN, NAN};
-    }
+    for (int u = 0; u < QT; ++u)
+        if (nan_blocks[u]) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+                if (nan_blocks[u] >> (dt / 2) & 1) o[u][dt] = f32x4_t{NAN, NAN, NAN, NAN};
+        }
 
-    // ---- the waves meet ----
-    __syncthreads();                             // (the staging rows become the waves' outputs)
-    float *s_o = reinterpret_cast<float *>(s_mem);
-    lsum = rows_sum(lsum);
-    if (gr == 0) { s_m[wave][n] = m; s_l[wave][n] = lsum; }
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t *>(s_o + (wave * 16 + n) * OP + dt * 16 + 4 * gr) = o[dt];
-    __syncthreads();
+    // ---- the waves meet, a tile of 16 queries at a time ----
+    float *s_o = reinterpret_cast<float *>(s_mem);               // (the staging rows become the waves' outputs)
     constexpr int TPQ = 4 * NW, EPT = D / TPQ;   // threads per query, and their elements, TPQ apart
-    const int oq = tid / TPQ, oe = tid % TPQ, orr = qt * 16 + oq;
-    float M = s_m[0][oq];
+    const int oq = tid / TPQ, oe = tid % TPQ;
+    const int q_first = qt * QT * 16;
+    auto store_out = [&](int q, const float (&acc)[EPT], float L) __attribute__((always_inline)) {
+        T *O = static_cast<T *>(a.O) + ((size_t)s * R + q_first + q) * D;
+        const float inv = 1.0f / L;                              // (no rows: 0 below; a NaN stays one)
 #pragma unroll
-    for (int w = 1; w < NW; ++w) M = fmaxf(M, s_m[w][oq]);
-    const float Mr = M == -INFINITY ? 0.f : M;
-    float L = 0.f, acc[EPT] = {};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        const float f = __builtin_amdgcn_exp2f(s_m[w][oq] - Mr);
-        L += s_l[w][oq] * f;
-#pragma unroll
-        for (int e = 0; e < EPT; ++e) acc[e] += s_o[(w * 16 + oq) * OP + oe + TPQ * e] * f;
-    }
-    // where query q of the unit's output begins
-    auto out_of = [&](int q) __attribute__((always_inline)) {
-        const int x = qt * 16 + q, xg = x / a.Tq;
-        return static_cast<T *>(a.O) + ((((size_t)lb * g.Hkv + h) * a.G + xg) * a.Tq + (x - xg * a.Tq)) * D;
+        for (int e = 0; e < EPT; ++e) Storage<T>::store(O + oe + TPQ * e, L == 0.f ? 0.f : acc[e] * inv);
     };
-    if (active == 1) {
-        if (orr < R) {
-            const float inv = 1.0f / L;                          // (no rows: 0 below; a NaN stays one)
-            T *O = out_of(oq);
 #pragma unroll
-            for (int e = 0; e < EPT; ++e) Storage<T>::store(O + oe + TPQ * e, L == 0.f ? 0.f : acc[e] * inv);
+    for (int u = 0; u < QT; ++u) {
+        __syncthreads();
+        const float lw = rows_sum(lsum[u]);
+        if (gr == 0) { s_m[wave][n] = m[u]; s_l[wave][n] = lw; }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t *>(s_o + (wave * 16 + n) * OP + dt * 16 + 4 * gr) = o[u][dt];
+        __syncthreads();
+        float M = s_m[0][oq];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) M = fmaxf(M, s_m[w][oq]);
+        const float Mr = M == -INFINITY ? 0.f : M;
+        float L = 0.f, acc[EPT] = {};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float f = __builtin_amdgcn_exp2f(s_m[w][oq] - Mr);
+            L += s_l[w][oq] * f;
+#pragma unroll
+            for (int e = 0; e < EPT; ++e) acc[e] += s_o[(w * 16 + oq) * OP + oe + TPQ * e] * f;
         }
-        return;
-    }
-    if (orr < R) {
-        float *part = a.part + (((size_t)unit * a.nsplit + split) * 16 + oq) * (D + 2);
+        const int q = u * 16 + oq;
+        if (q_first + q >= R) continue;
+        if (active == 1) {
+            store_out(q, acc, L);
+            continue;
+        }
+        float *part = a.part + (((size_t)unit * a.nsplit + split) * (16 * QT) + q) * (D + 2);
 #pragma unroll
         for (int e = 0; e < EPT; ++e) store_device(part + oe + TPQ * e, acc[e]);
         if (oe == 0) { store_device(part + D, M); store_device(part + D + 1, L); }
     }
+    if (active == 1) return;
     // ---- the workgroups meet: as in decode attention ----
     __shared__ int s_last;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // this wave's stores have completed
@@ -445,88 +482,86 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 ? 3 : 2) void pag
     if (tid == 0) __hip_atomic_store(a.tickets + unit, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     // Few queries leave most of the 16 rows of threads idle: those take partials side by side (row q + Q k: partials k, k + 16 / Q, ...
     // of query q), which are added up in LDS in that order.
-    const int live = min(16, R - qt * 16);
-    int lq = 0;
-    while (1 << lq < live) ++lq;
-    const int Q = 1 << lq, q = oq & (Q - 1), k0 = oq >> lq, kn = 16 >> lq;
-    L = 0.f;
-    M = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) acc[e] = 0.f;
-    if (q < live) {
-        const float *part = a.part + ((size_t)unit * a.nsplit * 16 + q) * (D + 2);
+    for (int u = 0; u < QT; ++u) {
+        const int live = min(16, R - q_first - u * 16);
+        if (live <= 0) return;
+        int lq = 0;
+        while (1 << lq < live) ++lq;
+        const int Q = 1 << lq, q = oq & (Q - 1), k0 = oq >> lq, kn = 16 >> lq;
+        float L = 0.f, M = -INFINITY, acc[EPT] = {};
+        if (q < live) {
+            const float *part = a.part + ((size_t)unit * a.nsplit * (16 * QT) + u * 16 + q) * (D + 2);
 #pragma unroll 2
-        for (int x = k0; x < active; x += kn) {
-            const float *pp = part + (size_t)x * 16 * (D + 2);
-            const float px = load_device(pp + D), pl = load_device(pp + D + 1);
-            float v[EPT];
+            for (int x = k0; x < active; x += kn) {
+                const float *pp = part + (size_t)x * (16 * QT) * (D + 2);
+                const float px = load_device(pp + D), pl = load_device(pp + D + 1);
+                float v[EPT];
 #pragma unroll
-            for (int e = 0; e < EPT; ++e) v[e] = load_device(pp + oe + TPQ * e);
-            const float Mn = fmaxf(M, px), ref = Mn == -INFINITY ? 0.f : Mn, f0 = __builtin_amdgcn_exp2f(M - ref), f1 = __builtin_amdgcn_exp2f(px - ref);
-            L = L * f0 + pl * f1;
+                for (int e = 0; e < EPT; ++e) v[e] = load_device(pp + oe + TPQ * e);
+                const float Mn = fmaxf(M, px), ref = Mn == -INFINITY ? 0.f : Mn, f0 = __builtin_amdgcn_exp2f(M - ref), f1 = __builtin_amdgcn_exp2f(px - ref);
+                L = L * f0 + pl * f1;
 #pragma unroll
-            for (int e = 0; e < EPT; ++e) acc[e] = acc[e] * f0 + v[e] * f1;
-            M = Mn;
+                for (int e = 0; e < EPT; ++e) acc[e] = acc[e] * f0 + v[e] * f1;
+                M = Mn;
+            }
         }
-    }
-    if (kn > 1) {
-        // (reads of s_o and s_m by the first merge lie behind the barriers of the ticket)
-        float *mm = &s_m[0][0], *ll = &s_l[0][0];
-        if (oe == 0) { mm[oq] = M; ll[oq] = L; }
+        if (kn > 1) {
+            // (the reads of s_o and s_m before lie behind the barriers of the ticket: only the unit's last tile has few queries)
+            float *mm = &s_m[0][0], *ll = &s_l[0][0];
+            if (oe == 0) { mm[oq] = M; ll[oq] = L; }
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) s_o[oq * OP + oe + TPQ * e] = acc[e];
-        __syncthreads();
-        if (k0 != 0) return;
-        M = -INFINITY;
-        for (int k = 0; k < kn; ++k) M = fmaxf(M, mm[q + Q * k]);
-        const float ref = M == -INFINITY ? 0.f : M;
-        L = 0.f;
+            for (int e = 0; e < EPT; ++e) s_o[oq * OP + oe + TPQ * e] = acc[e];
+            __syncthreads();
+            if (k0 != 0) return;
+            M = -INFINITY;
+            for (int k = 0; k < kn; ++k) M = fmaxf(M, mm[q + Q * k]);
+            const float ref = M == -INFINITY ? 0.f : M;
+            L = 0.f;
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) acc[e] = 0.f;
-        for (int k = 0; k < kn; ++k) {
-            const float f = __builtin_amdgcn_exp2f(mm[q + Q * k] - ref);
-            L += ll[q + Q * k] * f;
+            for (int e = 0; e < EPT; ++e) acc[e] = 0.f;
+            for (int k = 0; k < kn; ++k) {
+                const float f = __builtin_amdgcn_exp2f(mm[q + Q * k] - ref);
+                L += ll[q + Q * k] * f;
 #pragma unroll
-            for (int e = 0; e < EPT; ++e) acc[e] += s_o[(q + Q * k) * OP + oe + TPQ * e] * f;
+                for (int e = 0; e < EPT; ++e) acc[e] += s_o[(q + Q * k) * OP + oe + TPQ * e] * f;
+            }
         }
+        if (q < live) store_out(u * 16 + q, acc, L);
     }
-    if (q >= live) return;
-    T *O = out_of(q);
-    const float inv = 1.0f / L;
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) Storage<T>::store(O + oe + TPQ * e, L == 0.f ? 0.f : acc[e] * inv);
 #endif
 }
 
-template <typename T, int D, int NW, bool STREAM> static hipError_t launch_waves(const PageAttnArgs &a, hipStream_t st)
+template <typename T, int D, int NW, bool STREAM, int QT> static hipError_t launch_waves(const PageAttnArgs &a, hipStream_t st)
 {
     constexpr int lds = NW * wave_lds<D>();
     if (lds > 64 * 1024 - 2048) {
         static std::atomic<uint64_t> done{0};
-        const hipError_t e = allow_lds(page_attention_kernel<T, D, NW, STREAM>, lds, done);
+        const hipError_t e = allow_lds(page_attention_kernel<T, D, NW, STREAM, QT>, lds, done);
         if (e != hipSuccess) return e;
     }
     const dim3 grid((unsigned)((int64_t)a.g.L * a.g.B * a.g.Hkv * a.qtiles * a.nsplit));
-    hipLaunchKernelGGL((page_attention_kernel<T, D, NW, STREAM>), grid, dim3(64 * NW), lds, st, a);
+    hipLaunchKernelGGL((page_attention_kernel<T, D, NW, STREAM, QT>), grid, dim3(64 * NW), lds, st, a);
     return hipGetLastError();
 }
-template <typename T, int D, bool STREAM> static hipError_t launch_stream(const PageAttnArgs &a, int waves, hipStream_t st)
+template <typename T, int D, bool STREAM, int QT> static hipError_t launch_stream(const PageAttnArgs &a, int waves, hipStream_t st)
 {
-    switch (waves) {
-    case 1: return launch_waves<T, D, 1, STREAM>(a, st);
-    case 4: return launch_waves<T, D, 4, STREAM>(a, st);
-    default: return launch_waves<T, D, 8, STREAM>(a, st);
+    if (waves == 1) return launch_waves<T, D, 1, STREAM, QT>(a, st);
+    if constexpr (QT == 1) {
+        if (waves == 8) return launch_waves<T, D, 8, STREAM, QT>(a, st);
     }
+    return launch_waves<T, D, 4, STREAM, QT>(a, st);
 }
-template <typename T> static hipError_t launch_type(const PageAttnArgs &a, int waves, hipStream_t st)
+template <typename T, int QT> static hipError_t launch_type(const PageAttnArgs &a, int waves, hipStream_t st)
 {
-    if (a.g.d == 128) return a.stream ? launch_stream<T, 128, true>(a, waves, st) : launch_stream<T, 128, false>(a, waves, st);
-    return a.stream ? launch_stream<T, 64, true>(a, waves, st) : launch_stream<T, 64, false>(a, waves, st);
+    if (a.g.d == 128) return a.stream ? launch_stream<T, 128, true, QT>(a, waves, st) : launch_stream<T, 128, false, QT>(a, waves, st);
+    return a.stream ? launch_stream<T, 64, true, QT>(a, waves, st) : launch_stream<T, 64, false, QT>(a, waves, st);
 }
 
-hipError_t launch_page_attention(const PageAttnArgs &a, int dtype, int waves, hipStream_t st)
+hipError_t launch_page_attention(const PageAttnArgs &a, int dtype, int queries, int waves, hipStream_t st)
 {
-    return dtype == KVEV_F32 ? launch_type<float>(a, waves, st) : launch_type<bf16_t>(a, waves, st);
+    if (dtype == KVEV_F32) return launch_type<float, 1>(a, waves, st);
+    return queries == 32 ? launch_type<bf16_t, 2>(a, waves, st) : launch_type<bf16_t, 1>(a, waves, st);
 }
 
 }  // namespace kvev

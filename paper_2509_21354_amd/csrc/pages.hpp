@@ -79,7 +79,7 @@ struct PagesArgs {
 hipError_t launch_rotary(const RotaryArgs &a, int dtype, hipStream_t st);
 hipError_t launch_page_append(const PageRowsArgs &a, int dtype, hipStream_t st);
 hipError_t launch_page_read(const PageRowsArgs &a, int dtype, hipStream_t st);
-hipError_t launch_page_attention(const PageAttnArgs &a, int dtype, int waves, hipStream_t st);       // waves of a workgroup: 1, 4 or 8
+hipError_t launch_page_attention(const PageAttnArgs &a, int dtype, int queries, int waves, hipStream_t st);       // waves of a workgroup: 1, 4 or 8
 hipError_t launch_page_frame(const PageAttnArgs &a, int queries, hipStream_t st);      // bf16; queries per unit: 128 or 256
 hipError_t launch_pages_reserve(const PagesArgs &a, hipStream_t st);
 hipError_t launch_pages_fork(const PagesArgs &a, hipStream_t st);

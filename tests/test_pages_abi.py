@@ -194,6 +194,7 @@ def test_python_calls_say_what_is_wrong_with_a_tensor():
 def test_hooks():
     L, n = kb.lib(), ctypes.c_int()
     assert L.kvev_debug_page_frame_work(-1) == kb.ERR_INVALID_ARG and L.kvev_debug_page_frame_work(0) == kb.OK
+    assert L.kvev_debug_page_pair_units(-1) == kb.ERR_INVALID_ARG and L.kvev_debug_page_pair_units(0) == kb.OK
     sh, pg, r = _shape(), kb.make_pages(32, 10, 7), ctypes.byref(n)
     f = L.kvev_debug_page_form
     assert f(ctypes.byref(sh), ctypes.byref(pg), 1, r, r, r) == kb.OK

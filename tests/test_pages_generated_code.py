@@ -23,15 +23,16 @@ def test_partials_are_in_memory_before_the_ticket(tmp_path):
         if "page_attention_kernel" in n:
             one_wave = re.search(r"I[ft]Li\d+ELi1E", n)                         # has no barrier: the wait stands for it
             found[n] = waits_before_ticket(waited(lines) if one_wave else lines)
-    assert len(found) == 24 and all(ok is True for ok in found.values()), [n for n, ok in found.items() if ok is not True]
+    assert len(found) == 32 and all(ok is True for ok in found.values()), [n for n, ok in found.items() if ok is not True]
 
 
 @pytest.mark.parametrize("name,kernel,most", [("page_attention.hip", "page_attention_kernelIt", 168), ("page_frame.hip", "page_frame_kernel", 256)])
 def test_registers_are_not_spilt(name, kernel, most, tmp_path):
-    """Three waves of page_attention_kernel on a SIMD, two of page_frame_kernel: spills within a chunk cost most of what the kernels
+    """Three waves of page_attention_kernel on a SIMD (two with 32 queries), two of page_frame_kernel: spills within a chunk cost most of what the kernels
     gain (four waves of the first: 629 us against 367)."""
     asm = assembly(name, tmp_path)
     rows = [(n, int(v), int(s)) for n, v, s in re.findall(r"\.name:\s+(_Z\S+)(?:(?!\.name:)[\s\S])*?\.vgpr_count:\s+(\d+)\s+\.vgpr_spill_count:\s+(\d+)", asm)]
     rows = [r for r in rows if kernel in r[0]]
-    assert len(rows) == (12 if kernel.startswith("page_att") else 4)
-    assert all(v <= most and s == 0 for _, v, s in rows if "Li8E" not in _ or kernel.startswith("page_f")), rows
+    assert len(rows) == (20 if kernel.startswith("page_att") else 4)
+    most_of = {n: 256 if n.endswith("ELi2EEEvNS_12PageAttnArgsE") else most for n, _, _ in rows}
+    assert all(v <= most_of[n] and s == 0 for n, v, s in rows if "Li8E" not in n or kernel.startswith("page_f")), rows

@@ -210,7 +210,7 @@ def check_attention(c, Q, O, lengths, first=None, q_start=None, store=None, head
             vis = np.concatenate((np.ones((G, Tq, m), bool), vis), 2)
         want, E, S = ref.attention(q[l, b, h * G:(h + 1) * G].reshape(G * Tq, d), K, V, vis.reshape(G * Tq, -1), 1 / np.sqrt(d))
         got = o[l, b, h * G:(h + 1) * G].reshape(G * Tq, d)
-        bound = ref.attention_bound(want, E, S, n + m, d, dtype, kb.kvev_debug_page_form(sh, c.pages, Tq)[0] > 16)
+        bound = ref.attention_bound(want, E, S, n + m, d, dtype, kb.kvev_debug_page_form(sh, c.pages, Tq)[0] > 32)
         bad = ~(np.abs(got - want) <= bound)
         assert not bad.any(), (what, (l, b, h), np.argwhere(bad)[:4], got[bad][:4], want[bad][:4], bound[bad][:4])
 
@@ -291,6 +291,14 @@ def frames():
 
 
 @pytest.fixture
+def pairs():
+    """... and units of 32 queries."""
+    kb.kvev_debug_page_pair_units(1)
+    yield
+    kb.kvev_debug_page_pair_units(0)
+
+
+@pytest.fixture
 def streamed():
     """Rows are read with the non-temporal hint."""
     kb.kvev_debug_attn_stream_bytes(1)
@@ -317,7 +325,32 @@ def test_attention_of_frames(case, frames):
     attention_case(case, 128 if case[5] // case[6] * case[8] <= 128 else 256)
 
 
+PAIRS = [
+    ("bf16", 128, 16, 1, 1, 17, 1, [1], 1, False, 0),
+    ("bf16", 128, 32, 1, 2, 4, 4, [260, 90], 17, True, 0),
+    ("bf16", 64, 64, 1, 2, 4, 1, [500, 100], 5, True, 0),
+    ("bf16", 128, 64, 2, 1, 8, 2, [333], 8, False, 0),
+    ("bf16", 64, 32, 2, 2, 4, 2, [0, 45], 16, False, 130),
+    ("bf16", 128, 16, 1, 3, 4, 2, [40, 7, 300], 20, True, 30),
+    ("bf16", 128, 64, 1, 1, 32, 1, [2050], 1, False, 0),
+    ("bf16", 64, 128, 1, 2, 2, 1, [1500, 640], 33, True, 20),
+    ("bf16", 128, 256, 1, 2, 4, 2, [700, 1], 23, False, 0),
+    ("bf16", 128, 32, 1, 3, 3, 1, [90, 2, 257], 100, True, 70),
+]
+
+
+@pytest.mark.parametrize("case", PAIRS, ids=case_id)
+def test_attention_of_pairs_of_tiles(case, pairs):
+    attention_case(case, 32)
+
+
+@pytest.mark.parametrize("case", PAIRS[1::3], ids=case_id)
+def test_attention_of_pairs_streamed(case, pairs, streamed):
+    attention_case(case, 32)
+
+
 @pytest.mark.parametrize("dtype,L,B,Hkv,G,Tq,T,form", [
+    (torch.bfloat16, 24, 16, 8, 4, 5, 150, (32, 1, 1)), (torch.bfloat16, 4, 20, 8, 3, 9, 500, (32, 4, 1)), (torch.bfloat16, 2, 8, 8, 4, 8, 4100, (32, 4, 4)),
     (torch.bfloat16, 16, 12, 8, 2, 3, 150, (16, 1, 1)), (torch.bfloat16, 4, 24, 8, 1, 1, 600, (16, 4, 1)), (torch.float32, 16, 12, 8, 1, 1, 150, (16, 1, 1)),
     (torch.float32, 1, 33, 8, 2, 2, 200, (16, 4, 1)), (torch.bfloat16, 1, 2, 8, 1, 1, 3000, (16, 8, 6)), (torch.bfloat16, 1, 16, 8, 1, 1, 3000, (16, 4, 3))])
 def test_attention_by_waves(dtype, L, B, Hkv, G, Tq, T, form):
@@ -344,13 +377,15 @@ def test_attention_forms():
     pages = kb.make_pages(64, 1 << 12, 128)
     for (B, Hkv, G, Tq, T), form in {(16, 8, 4, 256, 8192): (256, 8, 1), (16, 8, 4, 4, 8192): (16, 4, 8), (1, 8, 4, 256, 4000): (256, 8, 8),
                                      (1, 8, 4, 256, 600): (16, 4, 1), (16, 8, 4, 32, 4000): (128, 4, 4), (1, 32, 1, 1, 4091): (16, 8, 8), (64, 8, 4, 1, 8192): (16, 4, 2),
-                                     (1, 32, 1, 1, 300): (16, 8, 1), (64, 32, 1, 1, 1000): (16, 1, 1), (64, 32, 1, 1, 8192): (16, 4, 1)}.items():
+                                     (1, 32, 1, 1, 300): (16, 8, 1), (64, 32, 1, 1, 1000): (16, 1, 1), (64, 32, 1, 1, 8192): (16, 4, 1), (64, 8, 4, 8, 4000): (32, 4, 1), (32, 8, 4, 8, 2100): (32, 4, 2),
+                                     (64, 32, 4, 8, 1000): (32, 1, 1), (32, 8, 4, 8, 300): (16, 4, 1), (16, 8, 4, 16, 8192): (32, 4, 2),
+                                     (16, 8, 4, 17, 8192): (128, 4, 4), (1, 8, 4, 8, 4000): (16, 8, 8)}.items():
         assert kb.kvev_debug_page_form(shape_of(1, B, Hkv * G, Hkv, T=T), pages, Tq) == form, (B, Hkv, G, Tq, T)
     assert kb.kvev_debug_page_form(shape_of(1, 16, 32, 8, T=8192, dtype=torch.float32), pages, 256)[0] == 16
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-def test_calls_of_every_size_take_one_workspace(dtype, frames):
+def test_calls_of_every_size_take_one_workspace(dtype, frames, pairs):
     """Prompts, decode steps and growing rows in turn: whatever a call leaves in the scratch, the next one finds its tickets at zero."""
     lengths = [5900, 1300, 64]
     sh = shape_of(1, 3, 8, 4, 64, dtype, 5900)
@@ -365,7 +400,7 @@ def test_calls_of_every_size_take_one_workspace(dtype, frames):
         want[Tq, T] = torch.full_like(Q[Tq], 9.0)
         ws = kb.alloc_workspace(kb.page_workspace_bytes(kb.OP_PAGE_ATTENTION, sh, c.pages, Tq), "cuda")
         kb.kvev_page_attention(sh, c.pages, Q[Tq], Tq, c.pool, c.table, c.length, want[Tq, T], ws)
-    assert len({queries for queries, _, runs in forms if runs > 1}) == (2 if dtype == torch.bfloat16 else 1), forms
+    assert len({queries for queries, _, runs in forms if runs > 1}) == (3 if dtype == torch.bfloat16 else 1), forms
     for turn in range(3):
         for Tq, T in random.Random(turn).sample(sizes, len(sizes)) + sizes:
             sh.T = T
@@ -440,6 +475,13 @@ def test_attention_scores_of_every_size(dtype, Tq, frames):
             c.read(ints([0, 0]), None, n, k, v)
             best = torch.matmul(k.double(), Q.double().transpose(3, 4).contiguous()).argmax(3)
             assert torch.equal(O, torch.gather(v, 3, best[..., None].expand(-1, -1, -1, -1, 128)))
+
+
+def test_pairs_of_tiles_in_the_same_places(pairs):
+    """Windows, hidden blocks that are not finite and scores of every size, as above."""
+    test_attention_over_a_window(40, None)
+    test_attention_keeps_what_is_hidden_apart(torch.bfloat16, 30, None)
+    test_attention_scores_of_every_size(torch.bfloat16, 60, None)
 
 
 def test_attention_of_a_long_cache():
