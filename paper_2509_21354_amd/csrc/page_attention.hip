@@ -308,11 +308,15 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 && QT == 1 ? 3 : 
         for (int h2 = 0; h2 < 2; ++h2) {
             if (NQ > 1 && h2 * 32 >= here) break;
             typename Terms<T>::Raw raw[2][KS];
+            auto load = [&](int i, int kk) __attribute__((always_inline)) {
+                Terms<T>::load(Vc + (size_t)min(ch * 64 + h2 * 32 + i * 16 + n, kept - 1) * D + gr * (D / 4) + kk * 8, raw[i][kk]);
+            };
+            if (NQ > 1) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int kk = 0; kk < KS; ++kk)
-                    Terms<T>::load(Vc + (size_t)min(ch * 64 + h2 * 32 + i * 16 + n, kept - 1) * D + gr * (D / 4) + kk * 8, raw[i][kk]);
+                    for (int kk = 0; kk < KS; ++kk) load(i, kk);
+            }
 #pragma unroll
             for (int x = NQ - 1; x >= 0; --x) {
 #pragma unroll
@@ -320,6 +324,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 && QT == 1 ? 3 : 
 #pragma unroll
                     for (int kk = 0; kk < KS; ++kk) {
                         bf16x8_t vf[NQ];
+                        if (NQ == 1) load(i, kk);
                         Terms<T>::cut(raw[i][kk], vf);
                         if (h2 * 32 + i * 16 + n >= here) vf[x] = __builtin_bit_cast(bf16x8_t, make_uint4(0u, 0u, 0u, 0u));
                         *reinterpret_cast<bf16x8_t *>(put[kk] + i * 16 * 2 * D) = vf[x];
