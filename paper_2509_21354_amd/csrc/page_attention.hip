@@ -64,7 +64,7 @@ __device__ __forceinline__ void cut3(const float (&x)[8], bf16x8_t (&t)[3])
     for (int k = 0; k < 3; ++k) t[k] = __builtin_bit_cast(bf16x8_t, make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]));
 }
 
-// weights (0 .. 1) as N bf16 terms: rounded, then what the rounding left
+// weights as N bf16 terms: rounded, then what the rounding left
 template <int N> __device__ __forceinline__ void cut_weights(const float (&p)[8], bf16x8_t (&t)[N])
 {
     float r[8];
@@ -213,9 +213,9 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 && QT == 1 ? 3 : 
 #pragma unroll
         for (int i = 5; i < 15; i += 2) mx = max3(mx, st[i / 4][i % 4], st[(i + 1) / 4][(i + 1) % 4]);
         mx = rows_max(fmaxf(mx, st[3][3])) * c;
-        const float m_new = fmaxf(m[u], mx), ref = m_new == -INFINITY ? 0.f : m_new;
-        if (__any(m_new > m[u])) {
-            const float alpha = __builtin_amdgcn_exp2f(m[u] - ref);
+        const float m_new = fmaxf(m[u], mx);
+        if (__any(m_new > m[u] + kSlack)) {
+            const float alpha = __builtin_amdgcn_exp2f(m[u] - (m_new == -INFINITY ? 0.f : m_new));
             lsum[u] *= alpha;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
@@ -223,6 +223,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 && QT == 1 ? 3 : 
                 for (int e = 0; e < 4; ++e) o[u][dt][e] *= alpha;
             m[u] = m_new;
         }
+        const float ref = m[u] == -INFINITY ? 0.f : m[u];
         // (The multiply-add leaves the rounding of the maximum's product in every weight, a factor that the normaliser shares.
         // Where it is no longer near 1, the products are rounded first.)
         float cc = c;

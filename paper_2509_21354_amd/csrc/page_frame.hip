@@ -29,6 +29,7 @@ template <int D> __device__ __forceinline__ int swizzle_v(int row)
     return D == 128 ? 4 * (row & 3) + ((row >> 2) & 3) : 4 * ((row >> 1) & 1) + ((row >> 2) & 3);
 }
 typedef __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 typedef __attribute__((address_space(3))) bf16x8_t lds_bf16x8_t;
 
 // The rows of a unit: the store's in tiles of 64, then the pages' from the tile of `first` up to the last token that some of its
@@ -275,6 +276,7 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : 1) void page_frame_kernel(
             __builtin_amdgcn_sched_barrier(0);
         });
         static_for<RING>(read_v);
+        const uint64_t marked = s_nan[slot][lane & 3];
         __builtin_amdgcn_sched_barrier(0);
         // register r of block kb is row 32 kb + 8 (r / 4) + 4 hh + r % 4 of the tile
         if (!full) {
@@ -303,9 +305,8 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : 1) void page_frame_kernel(
         my = mx;
         swap32(mx, my);
         mx = fmaxf(m, fmaxf(mx, my) * c);
-        const float ref = mx == -INFINITY ? 0.f : mx;
-        if (__any(mx > m)) {
-            const float alpha = __builtin_amdgcn_exp2f(m - ref);
+        if (__any(mx > m + kSlack)) {
+            const float alpha = __builtin_amdgcn_exp2f(m - (mx == -INFINITY ? 0.f : mx));
             m = mx;
             lsum *= alpha;
 #pragma unroll
@@ -313,6 +314,7 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : 1) void page_frame_kernel(
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
         }
+        const float ref = m == -INFINITY ? 0.f : m;
         float cc = c;
         if (__any(fabsf(ref) > 0x1p20f)) {       // (see page_attention.hip)
             cc = 1.0f;
@@ -327,9 +329,8 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : 1) void page_frame_kernel(
             constexpr int sx = decltype(sxc)::value, e = decltype(ec)::value;
             const float p0 = __builtin_amdgcn_exp2f(fmaf(st[sx >> 1][8 * (sx & 1) + 2 * e], cc, -ref));
             const float p1 = __builtin_amdgcn_exp2f(fmaf(st[sx >> 1][8 * (sx & 1) + 2 * e + 1], cc, -ref));
-            lsum += p0;
-            p_even += p1;
             pw[sx & 1][e] = pack_bf16x2(p0, p1);
+            (e & 1 ? p_even : lsum) = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pw[sx & 1][e]), __builtin_bit_cast(bf16x2_t, 0x3F803F80u), e & 1 ? p_even : lsum, false);
         };
         static_for<4>([&](auto ec) __attribute__((always_inline)) { weights(std::integral_constant<int, 0>{}, ec); });
         static_for<4 * DT>([&](auto ic) __attribute__((always_inline)) {
@@ -344,7 +345,7 @@ __global__ __launch_bounds__(64 * NWV, NWV == 4 ? 2 : 1) void page_frame_kernel(
             __builtin_amdgcn_sched_barrier(0);
         });
         lsum += p_even;
-        if (__any(s_nan[slot][lane & 3] != 0)) { // (rare)
+        if (__any(marked != 0)) {                // (rare)
             for (int i = 0; i < 4; ++i)
                 for (uint64_t bad = s_nan[slot][i]; bad; bad &= bad - 1) {
                     const int x = __builtin_ctzll(bad);

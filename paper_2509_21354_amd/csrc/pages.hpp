@@ -98,6 +98,9 @@ __host__ __device__ inline size_t reserve_words(const PageGeom &g) { return 64 +
 __host__ __device__ inline size_t compact_words(const PageGeom &g) { return 64 + (size_t)g.n_pages; }
 
 #ifdef __HIP_DEVICE_COMPILE__
+// A softmax's running maximum is a reference that weights are taken against, and stays while no score is more than kSlack above it
+// (in powers of two): what was summed is scaled seldom, weights reach 256, and no rounding depends on it but the fp32 exponent's.
+constexpr float kSlack = 8.0f;
 constexpr uint32_t kNanScale = 255;
 constexpr uint32_t kInfBits = 0x7F800000u;
 
