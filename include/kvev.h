@@ -354,7 +354,7 @@ int kvev_page_read(const kvev_shape *shape, const kvev_pages *pages, const void 
  * Scores, softmax and sums are fp32, O is rounded once.  fp32: operands enter the matrix cores as
  * three bf16 terms; bf16: the softmax weights as two, 16 significant bits, or as one rounded to
  * bf16 in frames (48 queries or more to a key-value head, and enough rows to pay for the form),
- * whose normaliser sums them unrounded as in kvev_gated_attention.  shape->T (0: the capacity)
+ * whose normaliser sums the rounded ones.  shape->T (0: the capacity)
  * says for what length of row the launch is made; any length is right, and results depend on it
  * in the order of sums and the choice of the form only.
  * Workspace: kvev_page_workspace_bytes(KVEV_OP_PAGE_ATTENTION, shape, pages, Tq), enough for every
