@@ -26,6 +26,8 @@ CASES = [  # dtype, L, B, H, Hkv, d, Tq, sections, layout
     ("bf16", 1, 1, 1, 1, 128, 1, (64,), 0), ("bf16", 1, 2, 4, 2, 128, 5, (16, 24, 24), 0), ("f32", 1, 2, 4, 4, 64, 9, (10, 11, 11), 0),
     ("bf16", 2, 1, 8, 1, 64, 33, (8, 8, 16), 1), ("f32", 2, 2, 3, 1, 128, 40, (16, 16, 16, 16), 1), ("bf16", 1, 3, 2, 2, 128, 70, (7, 9, 10), 0),
     ("f32", 1, 1, 5, 5, 64, 17, (1, 2), 1), ("bf16", 1, 1, 2, 1, 64, 300, (0, 32), 0), ("bf16", 1, 2, 4, 4, 128, 3, (1,), 1), ("f32", 1, 1, 2, 2, 128, 2, (3, 0, 2), 0),
+    ("bf16", 1, 2, 3, 1, 128, 37, (20, 20, 21), 0), ("f32", 2, 1, 3, 1, 64, 21, (10, 10, 11), 0), ("bf16", 1, 1, 1, 1, 64, 1, (31,), 0), ("f32", 1, 1, 1, 1, 64, 2, (31,), 0),
+    ("bf16", 1, 3, 5, 5, 64, 50, (1,), 0), ("f32", 1, 2, 9, 3, 128, 130, (20, 21, 22), 0), ("bf16", 2, 3, 12, 4, 128, 300, (3, 5, 9), 0),
     ("bf16", 3, 1, 40, 8, 128, 1, (24, 20, 20), 1), ("f32", 1, 2, 2, 2, 64, 31, (4, 4, 4, 4), 0)]
 
 
@@ -57,6 +59,27 @@ def test_rotary(case, inverse):
     assert torch.equal(only, ko)
     kb.kvev_rotary(*args, q, None, q, None, inverse)
     assert torch.equal(q, qo)
+
+
+@pytest.mark.parametrize("sections,layout", [((16, 24, 24), 0), ((7, 9, 10), 0), ((7, 9, 10), 1)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_values_that_are_not_finite_stay_in_their_pairs(dtype, sections, layout):
+    P, d, Tq = sum(sections), 128, 6
+    x = _draw(1, 1, 1, 2, Tq, d, dtype=dtype)
+    bad = x.clone()
+    for t, e in ((0, 0), (1, P - 1), (2, P), (3, 2 * P - 1), (4, d - 1), (5, 40)):
+        bad[..., t, e] = float("inf") if t % 2 else float("nan")
+    pos = torch.arange(1, 3 * Tq + 1, dtype=torch.int32).view(3, 1, Tq)
+    args = (_shape(1, 1, 2, 2, d, dtype), kb.make_rotary_axes(sections, layout), torch.linspace(0.1, 1, P).cuda(), pos.cuda(), Tq)
+    y, z = (torch.empty_like(x, device="cuda") for _ in range(2))
+    kb.kvev_rotary(*args, x.cuda(), None, y, None)
+    kb.kvev_rotary(*args, bad.cuda(), None, z, None)
+    y, z = y.cpu(), z.cpu()
+    pair = lambda e: (e,) if e >= 2 * P else (e, e ^ 1) if layout else (e, e + P if e < P else e - P)
+    for t, e in ((0, 0), (1, P - 1), (2, P), (3, 2 * P - 1), (4, d - 1), (5, 40)):
+        hit = torch.zeros(d, dtype=torch.bool)
+        hit[list(pair(e))] = True
+        assert not torch.isfinite(z[0, 0, :, t, hit]).any() and torch.equal(z[0, 0, :, t, ~hit], y[0, 0, :, t, ~hit])
 
 
 @pytest.mark.parametrize("layout", [0, 1])
