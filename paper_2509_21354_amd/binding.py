@@ -524,19 +524,25 @@ def kvev_pages_trim(shape: Shape, pages: Pages, rows, n, first, keep, table, len
 
 
 def kvev_pages_copy(shape: Shape, pages: Pages, pool, src, dst, n, status):
-    a = _Args("kvev_pages_copy", shape, pages)
-    st = lib().kvev_pages_copy(ctypes.byref(shape), ctypes.byref(pages), a.pool(pool), a.ints("src", src, n), a.ints("dst", dst, n), n,
-                               a.ints("status", status, 1), _stream())
-    _check(st, "kvev_pages_copy")
+    st = _native.pages_copy(shape, pages, pool, src, dst, n, status) if _native else None
+    if st is None:
+        a = _Args("kvev_pages_copy", shape, pages)
+        st = lib().kvev_pages_copy(ctypes.byref(shape), ctypes.byref(pages), a.pool(pool), a.ints("src", src, n), a.ints("dst", dst, n), n,
+                                   a.ints("status", status, 1), _stream())
+    if st:
+        _check(st, "kvev_pages_copy")
 
 
 def kvev_pages_compact(shape: Shape, pages: Pages, pool, table, refs, to: Pages, to_pool, to_table, to_refs, status, ws):
-    a = _Args("kvev_pages_compact", shape, pages)
-    wp, wn = a.scratch(ws)
-    st = lib().kvev_pages_compact(ctypes.byref(shape), ctypes.byref(pages), a.pool(pool), a.table(table), a.ints("refs", refs, pages.n_pages),
-                                  ctypes.byref(to), a.pool(to_pool, to, "to_pool"), a.table(to_table, "to_table"),
-                                  a.ints("to_refs", to_refs, to.n_pages), a.ints("status", status, 1), wp, wn, _stream())
-    _check(st, "kvev_pages_compact")
+    st = _native.pages_compact(shape, pages, pool, table, refs, to, to_pool, to_table, to_refs, status, ws) if _native else None
+    if st is None:
+        a = _Args("kvev_pages_compact", shape, pages)
+        wp, wn = a.scratch(ws)
+        st = lib().kvev_pages_compact(ctypes.byref(shape), ctypes.byref(pages), a.pool(pool), a.table(table), a.ints("refs", refs, pages.n_pages),
+                                      ctypes.byref(to), a.pool(to_pool, to, "to_pool"), a.table(to_table, "to_table"),
+                                      a.ints("to_refs", to_refs, to.n_pages), a.ints("status", status, 1), wp, wn, _stream())
+    if st:
+        _check(st, "kvev_pages_compact")
 
 
 def kvev_rotary(shape: Shape, axes: RotaryAxes, freq, pos, Tq, Q, K, Q_out, K_out, inverse=0):

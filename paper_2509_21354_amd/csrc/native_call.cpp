@@ -23,11 +23,12 @@ PyObject *g_shape_type, *g_rows_type, *g_tensor_type, *g_initialized, *g_get_dev
 PyObject *g_pages_type, *g_axes_type, *g_f32, *g_bf16, *g_i32, *g_u8;       // (bind_pages)
 PyObject *s_is_contiguous, *s_data_ptr, *s_numel, *s_ptr, *s_dtype, *s_get_device;
 
-enum Entry { kPool, kGate, kGatePrepared, kSelect, kGated, kDense, kRetain, kCompact, kPoolBytes, kAppend, kRead, kPageAttn, kReserve, kFork, kTrim, kRotary, kEntries };
+enum Entry { kPool, kGate, kGatePrepared, kSelect, kGated, kDense, kRetain, kCompact, kPoolBytes, kAppend, kRead, kPageAttn, kReserve, kFork, kTrim, kCopy, kCompactPages, kRotary, kEntries };
 const char *const kNames[kEntries] = {"kvev_chunk_pool", "kvev_lstm_gate", "kvev_lstm_gate_prepared", "kvev_select",
                                       "kvev_gated_attention", "kvev_dense_attention", "kvev_retain", "kvev_compact_attention",
                                       "kvev_page_pool_bytes", "kvev_page_append", "kvev_page_read", "kvev_page_attention",
-                                      "kvev_pages_reserve", "kvev_pages_fork", "kvev_pages_trim", "kvev_rotary"};
+                                      "kvev_pages_reserve", "kvev_pages_fork", "kvev_pages_trim", "kvev_pages_copy", "kvev_pages_compact",
+                                      "kvev_rotary"};
 void *g_entry[kEntries];
 
 // Arguments are read one after the other; the first that is not plain leaves `plain` false, an exception leaves `error` true,
@@ -36,8 +37,9 @@ struct Reader {
     PyObject *const *args;
     Py_ssize_t n, at = 0;
     bool plain = true, error = false;
-    Py_buffer shape_view{}, more_view{};
-    bool has_view = false, has_more = false;
+    Py_buffer shape_view{}, more_view[2]{};
+    bool has_view = false;
+    int more_views = 0;
     long device = -1;                      // current device, once stream() was asked
 
     Reader(PyObject *const *a, Py_ssize_t count, Py_ssize_t want) : args(a), n(count) { plain = g_shape_type && count == want; }
@@ -45,7 +47,7 @@ struct Reader {
     ~Reader()
     {
         if (has_view) PyBuffer_Release(&shape_view);
-        if (has_more) PyBuffer_Release(&more_view);
+        while (more_views > 0) PyBuffer_Release(&more_view[--more_views]);
     }
     bool ok() const { return plain && !error; }
     PyObject *next() { return args[at++]; }
@@ -60,16 +62,17 @@ struct Reader {
         if ((size_t)shape_view.len < sizeof(kvev_shape)) { plain = false; return nullptr; }
         return static_cast<const kvev_shape *>(shape_view.buf);
     }
-    // the struct that goes with the shape (kvev_pages, kvev_rotary_axes)
+    // a struct that goes with the shape (kvev_pages, kvev_rotary_axes; two at most)
     template <class S> const S *more(PyObject *type)
     {
         if (!ok()) return nullptr;
         PyObject *o = next();
         if (!type || (PyObject *)Py_TYPE(o) != type) { plain = false; return nullptr; }
-        if (PyObject_GetBuffer(o, &more_view, PyBUF_SIMPLE) != 0) { error = true; return nullptr; }
-        has_more = true;
-        if ((size_t)more_view.len < sizeof(S)) { plain = false; return nullptr; }
-        return static_cast<const S *>(more_view.buf);
+        Py_buffer &view = more_view[more_views];
+        if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) { error = true; return nullptr; }
+        ++more_views;
+        if ((size_t)view.len < sizeof(S)) { plain = false; return nullptr; }
+        return static_cast<const S *>(view.buf);
     }
     // a contiguous tensor of at least `least` elements of `dtype` on the current device (after stream()); what is not is left to
     // binding.py, which says so
@@ -474,6 +477,42 @@ PyObject *pages_trim(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+PyObject *pages_copy(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    PageReader r(args, n, 7);
+    if (!r.pages()) return r.run([] { return 0; });
+    void *pool = r.pool();
+    const Py_ssize_t lists = r.at;
+    r.at += 2;
+    const int count = r.integer();
+    const Py_ssize_t rest = r.at;
+    r.at = lists;
+    void *src = r.ints(count), *dst = r.ints(count);
+    r.at = rest;
+    void *status = r.ints(1);
+    return r.run([&] { return ENTRY(kCopy, kvev_pages_copy)(r.sh, r.pg, pool, (int32_t *)src, (int32_t *)dst, count, (int32_t *)status, r.st); });
+}
+
+PyObject *pages_compact(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    PageReader r(args, n, 11);
+    if (!r.pages()) return r.run([] { return 0; });
+    const kvev_pages *from = r.pg;
+    void *pool = r.pool(), *table = r.table(), *refs = r.refs();
+    const kvev_pages *to = r.more<kvev_pages>(g_pages_type);
+    if (!to) return r.run([] { return 0; });
+    r.pg = to;
+    void *to_pool = r.pool();
+    r.pg = from;
+    void *to_table = r.table(), *to_refs = r.ints(to->n_pages), *status = r.ints(1);
+    size_t bytes;
+    void *ws = r.bytes(bytes);
+    return r.run([&] {
+        return ENTRY(kCompactPages, kvev_pages_compact)(r.sh, from, pool, (int32_t *)table, (int32_t *)refs, to, to_pool, (int32_t *)to_table, (int32_t *)to_refs,
+                                                        (int32_t *)status, ws, bytes, r.st);
+    });
+}
+
 PyObject *rotary(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     PageReader r(args, n, 10);
@@ -531,7 +570,7 @@ PyMethodDef g_methods[] = {
     FAST("gated_attention", gated_attention), FAST("dense_attention", dense_attention), FAST("retain", retain),
     FAST("compact_attention", compact_attention), FAST("page_append", page_append), FAST("page_read", page_read),
     FAST("page_attention", page_attention), FAST("pages_reserve", pages_reserve), FAST("pages_fork", pages_fork), FAST("pages_trim", pages_trim),
-    FAST("rotary", rotary), {"bind_pages", bind_pages, METH_VARARGS, nullptr}, {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+    FAST("pages_copy", pages_copy), FAST("pages_compact", pages_compact), FAST("rotary", rotary), {"bind_pages", bind_pages, METH_VARARGS, nullptr}, {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", "Marshalling of calls into libkvev.so.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

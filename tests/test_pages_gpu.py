@@ -807,3 +807,28 @@ def test_python_calls_by_either_way(monkeypatch):
             kb.kvev_page_append(sh, c.pages, K, V.transpose(2, 3).contiguous().transpose(2, 3), 70, c.start, None, c.table, c.pool)
     for x, y in zip(*outs):
         assert torch.equal(x, y)
+
+
+def test_copies_and_compaction_by_either_way(monkeypatch):
+    sh, outs = shape_of(B=2, H=4, H_kv=2), []
+    to = kb.make_pages(32, 6, 8)
+    for native in (kb._native, None):
+        monkeypatch.setattr(kb, "_native", native)
+        c = cache_of(sh, 32, [70, 33])
+        fill(c, [70, 33], torch.bfloat16)
+        free = [p for p in range(c.pages.n_pages) if not c.refs[p]]
+        kb.kvev_pages_copy(sh, c.pages, c.pool, ints([int(c.table[0, 0]), 99]), ints([free[0], free[1]]), 2, c.status)
+        pool, table, refs = torch.zeros(kb.page_pool_bytes(sh, to), dtype=torch.uint8, device="cuda"), torch.full_like(c.table, 7), ints([5] * 6)
+        to.max_pages = c.pages.max_pages
+        ws = kb.alloc_workspace(kb.page_workspace_bytes(kb.OP_PAGES_COMPACT, sh, c.pages, 0), "cuda")
+        kb.kvev_pages_compact(sh, c.pages, c.pool, c.table, c.refs, to, pool, table, refs, c.status, ws)
+        outs.append([c.pool.clone(), pool, table, refs, c.status.clone()])
+        assert int(c.status[0]) == 4 and (refs > 0).sum() == 5
+        with pytest.raises(kb.KvevError, match="to_pool has to hold"):
+            kb.kvev_pages_compact(sh, c.pages, c.pool, c.table, c.refs, to, pool[:-16], table, refs, c.status, ws)
+        with pytest.raises(kb.KvevError, match="to_refs has to hold 6 elements"):
+            kb.kvev_pages_compact(sh, c.pages, c.pool, c.table, c.refs, to, pool, table, refs[:5], c.status, ws)
+        with pytest.raises(kb.KvevError, match="src has to hold 2 elements"):
+            kb.kvev_pages_copy(sh, c.pages, c.pool, ints([0]), ints([1, 2]), 2, c.status)
+    for x, y in zip(*outs):
+        assert torch.equal(x, y)
