@@ -4,7 +4,7 @@
 // block's largest magnitude (as a bit pattern: an infinity or NaN is then simply the largest) is found by two exchanges within
 // the four lanes; the codes are rounded by the hardware conversion (to nearest, ties to even; division by a power of two is
 // exact), so a row read back is the same bits on every path.  Read: a word of codes and a scale byte per lane.
-// Both move bytes and little else: 2 d elements in, d + d / 16 bytes out per token and head, or back.  4 rows of 6000 - 8000 tokens x 8 heads, bf16,
+// Both move bytes and little else: 2 d elements in, d + d / 16 bytes out per token and head, or back.  4 rows of 5000 - 8000 tokens x 8 heads, bf16,
 // d = 128: 23.3 us in, 22.4 out, 5.8 and 6.0 TB/s (a large copy: 4.9; half of it lies in the memory-side cache).  One token of 64 rows x 8 heads: 2.9
 // and 2.6 us, the launch.
 #include "kernels.hpp"
