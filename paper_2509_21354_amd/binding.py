@@ -560,7 +560,7 @@ def kvev_rotary(shape: Shape, axes: RotaryAxes, freq, pos, Tq, Q, K, Q_out, K_ou
 
 class PagedCache:
     """Caller-owned buffers of one paged 4-bit cache (pool, page table, lengths, holders of each page, scratch).
-    Allocation only; no arithmetic."""
+    Allocation only; no arithmetic.  Tq: the most queries that attend() will be given."""
 
     def __init__(self, shape: Shape, page: int, n_pages: int, max_pages: int, Tq: int = 1, device="cuda"):
         self.shape, self.pages = shape, make_pages(page, n_pages, max_pages)
