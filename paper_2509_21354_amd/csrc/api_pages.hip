@@ -62,7 +62,9 @@ static size_t pool_bytes(const PageGeom &g) { return (size_t)g.L * g.n_pages * p
 // head: 512 heads x 200 tokens 13.3 and 11.2, x 4000 110 and 73; 256 x 300 9.2 and 10.4, x 1000 17.6 and 16.6, x 4000 54 and 42; 128 x
 // 4000 33.8 and 28.2, of 16 ragged rows up to 8192 36.6 and 39.1; 32 x 4000 15.6 and 19.4).  Their runs give every compute unit two
 // workgroups, all that it holds at once (four: 81 and 47 at 512 and 256 heads x 4000).
-// Frames (page_frame.hip; bf16): units of 128 or 256 queries, two workgroups or one per compute unit.  They take calls with 48 queries
+// Frames (page_frame.hip; bf16): units of 128 or, for more queries at d = 128, 256, two workgroups or one per compute unit.  At d = 64 the
+// registers of 128 queries fit three times, which gives more than converting a row for 256 at once (16 x 8 heads x 1024 queries x 8192
+// tokens 353 us, with 256 queries 386; one row of 4096 causal tokens 92 and 110).  Frames take calls with 48 queries
 // or more to a key-value head (65 where units of 32 are taken: 128 heads x 64 queries x 8192 tokens 70 and 84, 512 x 64 x 600
 // 32.3 and 29.4) and enough work (units of 16 queries x tokens; 4 query heads to a key-value head, units of 16 and frame, us):
 // 128 x 128 x 600 23.7 and 22.1; 128 x 256 x 600 32.6 and 29.0; 8 x 1024 x 4000 45.7 and 38.6; but 8 x 1024 x 600 12.1 and 22.2, 8 x 256
@@ -81,7 +83,7 @@ static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int 
     p.queries = queries;
     p.qtiles = (int)((R + p.queries - 1) / p.queries);
     p.units = (int64_t)g.L * g.B * g.Hkv * p.qtiles;
-    const int64_t chunks = (tokens + kPageChunk - 1) / kPageChunk, slots = p.queries == 128 ? 2 * cus : cus;
+    const int64_t chunks = (tokens + kPageChunk - 1) / kPageChunk, slots = p.queries == 128 ? (g.d == 64 ? 3 : 2) * cus : cus;
     auto fill = [&](int64_t wgs) { return (chunks * p.units + wgs - 1) / wgs; };       // the run of which `wgs` workgroups take all
     int64_t run;
     if (frame) {
@@ -136,7 +138,7 @@ static PageAttnPlan plan_page_attn(const kvev_shape *sh, const PageGeom &g, int 
     const bool pair = pairs > 0 ? p.units >= pairs : p.units >= 2 * cus || (2 * p.units >= cus && p.units * tokens >= kPairWork * cus);
     if (pair) best = p;
     if (R >= kFrameQueries) {
-        const PageAttnPlan f = plan_page_form(sh, g, Tq, tokens, R <= 128 ? 128 : 256);
+        const PageAttnPlan f = plan_page_form(sh, g, Tq, tokens, R <= 128 || g.d == 64 ? 128 : 256);
         any = std::max(any, f.ws_any);
         if (work >= g_frame_work.load() && !(pair && R <= kPairMost)) best = f;
     }

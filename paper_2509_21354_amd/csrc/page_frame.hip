@@ -437,8 +437,8 @@ template <int D, int NWV> static hipError_t launch_frame_as(const PageAttnArgs &
 
 hipError_t launch_page_frame(const PageAttnArgs &a, int queries, hipStream_t st)
 {
-    if (a.g.d == 128) return queries == 256 ? launch_frame_as<128, 8>(a, st) : launch_frame_as<128, 4>(a, st);
-    return queries == 256 ? launch_frame_as<64, 8>(a, st) : launch_frame_as<64, 4>(a, st);
+    if (a.g.d == 64) return launch_frame_as<64, 4>(a, st);
+    return queries == 256 ? launch_frame_as<128, 8>(a, st) : launch_frame_as<128, 4>(a, st);
 }
 
 }  // namespace kvev

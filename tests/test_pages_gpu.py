@@ -322,7 +322,7 @@ def test_attention_streamed(case, streamed):
 
 @pytest.mark.parametrize("case", FRAMES, ids=case_id)
 def test_attention_of_frames(case, frames):
-    attention_case(case, 128 if case[5] // case[6] * case[8] <= 128 else 256)
+    attention_case(case, 128 if case[1] == 64 or case[5] // case[6] * case[8] <= 128 else 256)
 
 
 PAIRS = [
