@@ -62,7 +62,9 @@ static size_t pool_bytes(const PageGeom &g) { return (size_t)g.L * g.n_pages * p
 // head: 512 heads x 200 tokens 13.3 and 11.2, x 4000 110 and 73; 256 x 300 9.2 and 10.4, x 1000 17.6 and 16.6, x 4000 54 and 42; 128 x
 // 4000 33.8 and 28.2, of 16 ragged rows up to 8192 36.6 and 39.1; 32 x 4000 15.6 and 19.4).  Their runs give every compute unit two
 // workgroups, all that it holds at once (four: 81 and 47 at 512 and 256 heads x 4000).
-// Frames (page_frame.hip; bf16): units of 128 or, for more queries at d = 128, 256, two workgroups or one per compute unit.  At d = 64 the
+// Frames (page_frame.hip; bf16): units of 128 or, for more queries at d = 128, 256, two workgroups or one per compute unit, whichever
+// takes less by the count of rounds (256 and 128, us: 128 heads x 292 queries x 4000 tokens 122 and 139, 512 x 292 x 600 101 and 78, 32 x
+// 580 x 4000 72 and 62, 128 x 1024 x 8192 521 and 573).  At d = 64 the
 // registers of 128 queries fit three times, which gives more than converting a row for 256 at once (16 x 8 heads x 1024 queries x 8192
 // tokens 353 us, with 256 queries 386; one row of 4096 causal tokens 92 and 110).  Frames take calls with 48 queries
 // or more to a key-value head (65 where units of 32 are taken: 128 heads x 64 queries x 8192 tokens 70 and 84, 512 x 64 x 600
@@ -74,10 +76,10 @@ constexpr int64_t kFrameWork = 1200000;
 constexpr int64_t kPairWork = 2000, kPairMost = 64;
 static std::atomic<int64_t> g_frame_work{kFrameWork};      // (kvev_debug_page_frame_work lowers it)
 static std::atomic<int64_t> g_pair_units{0};               // (kvev_debug_page_pair_units: 0: by the rule)
-struct PageAttnPlan { int queries, waves, qtiles, nsplit, run; int64_t units; size_t ticket_bytes, ws_bytes, ws_any; };
+struct PageAttnPlan { int queries, waves, qtiles, nsplit, run; int64_t units; size_t ticket_bytes, ws_bytes, ws_any; double time; };
 static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int Tq, int64_t tokens, int queries)
 {
-    PageAttnPlan p;
+    PageAttnPlan p{};
     const int64_t R = (int64_t)(sh->H / g.Hkv) * Tq, cus = device_compute_units(), cap = (int64_t)g.max_pages << g.page_shift;
     const bool frame = queries > 32;
     p.queries = queries;
@@ -89,8 +91,8 @@ static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int 
     if (frame) {
         p.waves = p.queries / 32;
         // as many runs as give the least time: rounds of workgroups, each run two tiles longer for its beginning and end, a tile of
-        // 64 rows 2.2 us (d = 128, 256 queries), partials out and in at 4 TB/s and a launch
-        const double tile = 2.2 * g.d / 128, merge = 2.0 * p.queries * (g.d + 4) * sizeof(float) / 4e6;
+        // 64 rows 2.2 us (d = 128; 2.4 for two workgroups of 128 queries), partials out and in at 4 TB/s and a launch
+        const double tile = (queries == 128 ? 2.4 : 2.2) * g.d / 128, merge = 2.0 * p.queries * (g.d + 4) * sizeof(float) / 4e6;
         double least = 0;
         int64_t best = 1;
         for (int64_t n = 1; n <= std::min<int64_t>(kPageMaxSplit, (chunks + 3) / 4) && (n == 1 || p.units * n <= kFrameRounds * slots); ++n) {
@@ -99,6 +101,7 @@ static PageAttnPlan plan_page_form(const kvev_shape *sh, const PageGeom &g, int 
             if (n == 1 || t < least) { least = t; best = n; }
         }
         run = (chunks + best - 1) / best;
+        p.time = least;
     } else if (queries == 16 && (sh->dtype == KVEV_F32 ? p.units <= cus : p.units * ((chunks + 7) / 8) <= cus)) {
         p.waves = 8;
         const int64_t n = std::max<int64_t>(cus / p.units, 1);
@@ -138,8 +141,13 @@ static PageAttnPlan plan_page_attn(const kvev_shape *sh, const PageGeom &g, int 
     const bool pair = pairs > 0 ? p.units >= pairs : p.units >= 2 * cus || (2 * p.units >= cus && p.units * tokens >= kPairWork * cus);
     if (pair) best = p;
     if (R >= kFrameQueries) {
-        const PageAttnPlan f = plan_page_form(sh, g, Tq, tokens, R <= 128 || g.d == 64 ? 128 : 256);
+        PageAttnPlan f = plan_page_form(sh, g, Tq, tokens, 128);
         any = std::max(any, f.ws_any);
+        if (R > 128 && g.d == 128) {
+            const PageAttnPlan w = plan_page_form(sh, g, Tq, tokens, 256);
+            any = std::max(any, w.ws_any);
+            if (w.time <= f.time) f = w;
+        }
         if (work >= g_frame_work.load() && !(pair && R <= kPairMost)) best = f;
     }
     best.ws_any = any;
