@@ -4,8 +4,8 @@
 // order.  Whoever needs pages takes the free ones of lowest index, in the order of the rows, so a call's outcome depends on
 // nothing but what the arrays held before it.  Atomics are integer additions and exchanges whose order does not show.
 // Tables and counts are small (a few bytes per page): those kernels are chains of memory round trips, one workgroup each where
-// they have to see all rows (16 rows, 560 pages: reserve 6.2 us, its copies 6.6, fork 4.3, trim 4.1; compaction's ranks of 21 000 pages 8).  Copies
-// move whole 16-byte pieces at the rate of the memory (compaction of 1.7 GB in and out: 358 us, 4.8 TB/s; a large copy: 4.9).
+// they have to see all rows (16 rows, 560 pages: reserve 6.2 us, its copies 6.6, fork 4.3, trim 4.1; compaction's ranks of 5 200 pages 8).  Copies
+// move whole 16-byte pieces at the rate of the memory (compaction of 1.7 GB in and out: 318 us, 5.4 TB/s; a large copy: 4.9).
 #include "kernels.hpp"
 #include "pages.hpp"
 
@@ -262,12 +262,12 @@ __global__ __launch_bounds__(256) void copy_kernel(PagesArgs a)
     }
 }
 
-// The place of every page in use among those in use (or -1), and the counts in their new order; word 0 of the scratch: whether
-// they fit.
+// The place of every page in use among those in use (or -1), the pages in use, and the counts in their new order; words 0 and 1 of
+// the scratch: whether they fit, and their number.
 __global__ __launch_bounds__(1024) void compact_rank_kernel(PagesArgs a)
 {
     const PageGeom &g = a.g;
-    int32_t *rank = a.ws + kHead;
+    int32_t *rank = a.ws + kHead, *list = rank + g.n_pages;
     int used = 0;
     constexpr int PER = 8;
     for (int64_t p0 = 0; p0 < g.n_pages; p0 += 1024 * PER) {
@@ -280,13 +280,18 @@ __global__ __launch_bounds__(1024) void compact_rank_kernel(PagesArgs a)
         at += used;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            if (p + i < g.n_pages) rank[p + i] = bits >> i & 1 ? at++ : -1;
+            if (p + i < g.n_pages) {
+                const bool in = bits >> i & 1;
+                rank[p + i] = in ? at : -1;
+                if (in) list[at++] = (int)p + i;
+            }
         used += sum;
     }
     __syncthreads();
     const bool fits = used <= a.to_pages;
     if (threadIdx.x == 0) {
         a.ws[0] = fits;
+        a.ws[1] = used;
         if (!fits) atomicOr(a.status, kStatusNoPages);
     }
     if (!fits) return;
@@ -295,22 +300,28 @@ __global__ __launch_bounds__(1024) void compact_rank_kernel(PagesArgs a)
     for (int p = used + threadIdx.x; p < a.to_pages; p += 1024) a.to_refs[p] = 0;
 }
 
+// The pages in use in parts of 32 KiB, dealt out evenly: few large pages are enough for the chip, and pages that are free cost nothing
+// (1.7 GB in and out 360 -> 318 us, 129 pages of 557 KB 33 -> 27.5; parts of 16 KiB 316 and 27.5, but 11.9 for 9.3 where pages are small).
+constexpr size_t kPart = 32768;
 template <bool STREAM> __global__ __launch_bounds__(256) void compact_copy_kernel(PagesArgs a)
 {
     if (!a.ws[0]) return;
     const PageGeom &g = a.g;
     const int32_t *rank = a.ws + kHead;
     const size_t block = block_bytes(g);
-    const int64_t cells = (int64_t)g.B * g.max_pages, units = (int64_t)g.n_pages * g.L;
+    const int64_t cells = (int64_t)g.B * g.max_pages;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < cells; i += (int64_t)gridDim.x * 256) {
         const int page = a.table[i];
         a.to_table[i] = (uint32_t)page < (uint32_t)g.n_pages ? rank[page] : -1;
     }
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int l = (int)(u / g.n_pages), p = (int)(u - (int64_t)l * g.n_pages), to = rank[p];
-        if (to < 0) continue;
-        copy_pieces<256, STREAM>(a.to_pool + ((size_t)l * a.to_pages + to) * g.Hkv * block, a.pool + ((size_t)l * g.n_pages + p) * g.Hkv * block,
-                                 g.Hkv * block, threadIdx.x);
+    const int32_t *list = rank + g.n_pages;
+    const int used = a.ws[1];
+    const size_t bytes = g.Hkv * block, parts = (bytes + kPart - 1) / kPart, units = (size_t)used * g.L * parts;
+    for (size_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const size_t q = u / parts, at = (u - q * parts) * kPart;
+        const int l = (int)(q / (uint32_t)used), to = (int)(q - (size_t)l * used), p = list[to];
+        copy_pieces<256, STREAM>(a.to_pool + ((size_t)l * a.to_pages + to) * bytes + at, a.pool + ((size_t)l * g.n_pages + p) * bytes + at,
+                                 bytes - at < kPart ? bytes - at : kPart, threadIdx.x);
     }
 }
 
@@ -345,7 +356,8 @@ hipError_t launch_pages_compact(const PagesArgs &a, hipStream_t st)
     hipLaunchKernelGGL(compact_rank_kernel, dim3(1), dim3(1024), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const dim3 grid(grid_of((int64_t)a.g.n_pages * a.g.L, 2048));
+    const int64_t parts = (int64_t)((a.g.Hkv * block_bytes(a.g) + kPart - 1) / kPart);
+    const dim3 grid(grid_of((a.g.n_pages < 2048 ? (int64_t)a.g.n_pages * a.g.L : 2048) * parts, 2048));
     if (a.stream) hipLaunchKernelGGL((compact_copy_kernel<true>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((compact_copy_kernel<false>), grid, dim3(256), 0, st, a);
     return hipGetLastError();

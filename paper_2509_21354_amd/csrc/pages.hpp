@@ -95,7 +95,8 @@ __host__ __device__ inline size_t page_bytes(const PageGeom &g) { return (size_t
 // int32 words of scratch: what a row needs and where it begins in the list of pages found, rows to copy (from, to, groups), their
 // number; the list
 __host__ __device__ inline size_t reserve_words(const PageGeom &g) { return 64 + (size_t)5 * g.B + g.n_pages; }
-__host__ __device__ inline size_t compact_words(const PageGeom &g) { return 64 + (size_t)g.n_pages; }
+// a head; places of all pages; the pages in use
+__host__ __device__ inline size_t compact_words(const PageGeom &g) { return 64 + 2 * (size_t)g.n_pages; }
 
 #ifdef __HIP_DEVICE_COMPILE__
 // A softmax's running maximum is a reference that weights are taken against, and stays while no score is more than kSlack above it
