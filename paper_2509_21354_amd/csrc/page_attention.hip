@@ -27,6 +27,10 @@
 // token's scores NaN, which a query that must not see the token replaces.  Values would reach every query of the tile as 0 * NaN,
 // so blocks of values marked 255 enter the product as zeros, and the outputs of the queries that do see the token are set to NaN
 // at the end.
+// Summaries of the store are seen by every query, so a NaN among them may go through the products.  An infinity may not: an operand that
+// is cut into terms multiplies it term by term, and a term that is zero, or of the other sign, makes a NaN of what should be an
+// infinity.  A wave whose sums are NaN behind its rows of the store takes these rows again, with what is not finite apart: zeros in its place in the
+// products of all terms, then a product of its own with the other operand's first term, which has the operand's sign.
 #include "kernels.hpp"
 #include "pages.hpp"
 #include <atomic>
@@ -89,12 +93,38 @@ template <> struct Terms<bf16_t> {
     struct Raw { bf16x8_t v; };                  // 8 elements as they lie in memory
     static __device__ __forceinline__ void load(const bf16_t *p, Raw &r) { r.v = *reinterpret_cast<const bf16x8_t *>(p); }
     static __device__ __forceinline__ void cut(const Raw &r, bf16x8_t (&t)[1]) { t[0] = r.v; }
+    // what is not finite, with zeros in the other places; `r` keeps the rest
+    static __device__ __forceinline__ bf16x8_t take_infinite(Raw &r)
+    {
+        const u32x4_t w = __builtin_bit_cast(u32x4_t, r.v);
+        u32x4_t far;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = (w[i] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u, hi = (w[i] & kInfBits) == kInfBits ? 0xFFFF0000u : 0u;
+            far[i] = w[i] & (lo | hi);
+        }
+        r.v = __builtin_bit_cast(bf16x8_t, w ^ far);
+        return __builtin_bit_cast(bf16x8_t, far);
+    }
 };
 template <> struct Terms<float> {
     static constexpr int Q = 3, P = 3;
     struct Raw { float v[8]; };
     static __device__ __forceinline__ void load(const float *p, Raw &r) { VecLoad<float, 8>::run(p, r.v); }
     static __device__ __forceinline__ void cut(const Raw &r, bf16x8_t (&t)[3]) { cut3(r.v, t); }
+    static __device__ __forceinline__ bf16x8_t take_infinite(Raw &r)
+    {
+        Raw far;
+        bf16x8_t t[3];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bool finite = (__float_as_uint(r.v[e]) & kInfBits) != kInfBits;
+            far.v[e] = finite ? 0.f : r.v[e];
+            if (!finite) r.v[e] = 0.f;
+        }
+        cut3(far.v, t);
+        return t[0];
+    }
 };
 
 // where in a group's keys or values lane (token n, quarter gr) finds its codes
@@ -184,14 +214,17 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 && QT == 1 ? 3 : 
     float m[QT], lsum[QT];                       // scaled running maximum and this lane's part of the sum, of query n of each tile
     f32x4_t o[QT][DT];
     uint32_t nan_blocks[QT];                     // blocks of d whose values are NaN in a token that the query sees
+    auto reset = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < QT; ++u) {
-        m[u] = -INFINITY;
-        lsum[u] = 0.f;
-        nan_blocks[u] = 0;
+        for (int u = 0; u < QT; ++u) {
+            m[u] = -INFINITY;
+            lsum[u] = 0.f;
+            nan_blocks[u] = 0;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[u][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
+            for (int dt = 0; dt < DT; ++dt) o[u][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+    };
+    reset();
 
     // staging: lane (n, gr) writes pieces gr * KS + kk of tokens n and 16 + n; it reads, of tokens 4 gr + n / 4 and 16 further on, piece
     // 2 dt + (n & 3) / 2, half n & 1
@@ -272,66 +305,106 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 && QT == 1 ? 3 : 
     // ---- rows of the store ----
     // (fp32: cutting a row into terms is most of the work, so half chunks without rows are passed over and values are read once for all
     // terms: 16 summaries of 2 x 4 heads x 33 queries add 0.4 us to 6.8, 3.5 without)
-    int ch = c0 + wave;
-    for (; ch < min(sc, c1); ch += NW) {
-        f32x4_t st[QT][4];
-        bf16x8_t pb[QT][2][NP];
-        const T *Kc = static_cast<const T *>(a.Kc) + (size_t)s * a.k_cap * D, *Vc = static_cast<const T *>(a.Vc) + (size_t)s * a.k_cap * D;
-        const int here = kept - ch * 64;         // rows of this chunk (1 and more)
+    // (APART: what is not finite by itself)
+    int ch;
+    auto store_rows = [&](auto apart) __attribute__((always_inline)) {
+        constexpr bool APART = decltype(apart)::value;
+        for (ch = c0 + wave; ch < min(sc, c1); ch += NW) {
+            f32x4_t st[QT][4];
+            bf16x8_t pb[QT][2][NP];
+            const T *Kc = static_cast<const T *>(a.Kc) + (size_t)s * a.k_cap * D, *Vc = static_cast<const T *>(a.Vc) + (size_t)s * a.k_cap * D;
+            const int here = kept - ch * 64;         // rows of this chunk (1 and more)
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
+            for (int kt = 0; kt < 4; ++kt) {
 #pragma unroll
-            for (int u = 0; u < QT; ++u) st[u][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            if (NQ == 1 || kt / 2 * 32 < here) {
-#pragma unroll
-                for (int kk = 0; kk < KS; ++kk) {
-                    typename Terms<T>::Raw raw;
-                    bf16x8_t kf[NQ];
-                    Terms<T>::load(Kc + (size_t)min(ch * 64 + kt * 16 + n, kept - 1) * D + gr * (D / 4) + kk * 8, raw);
-                    Terms<T>::cut(raw, kf);
-#pragma unroll
-                    for (int u = 0; u < QT; ++u)
-#pragma unroll
-                        for (int x = NQ - 1; x >= 0; --x)
-#pragma unroll
-                            for (int y = NQ - 1 - x; y >= 0; --y) st[u][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x], qf[u][kk][y], st[u][kt], 0, 0, 0);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < QT; ++u)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (kt * 16 + 4 * gr + e >= here) st[u][kt][e] = -INFINITY;
-        }
-#pragma unroll
-        for (int u = 0; u < QT; ++u) soft(u, st[u], pb[u]);
-#pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2) {
-            if (NQ > 1 && h2 * 32 >= here) break;
-            typename Terms<T>::Raw raw[2][KS];
-            auto load = [&](int i, int kk) __attribute__((always_inline)) {
-                Terms<T>::load(Vc + (size_t)min(ch * 64 + h2 * 32 + i * 16 + n, kept - 1) * D + gr * (D / 4) + kk * 8, raw[i][kk]);
-            };
-            if (NQ > 1) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int kk = 0; kk < KS; ++kk) load(i, kk);
-            }
-#pragma unroll
-            for (int x = NQ - 1; x >= 0; --x) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int u = 0; u < QT; ++u) st[u][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                if (NQ == 1 || kt / 2 * 32 < here) {
 #pragma unroll
                     for (int kk = 0; kk < KS; ++kk) {
-                        bf16x8_t vf[NQ];
-                        if (NQ == 1) load(i, kk);
-                        Terms<T>::cut(raw[i][kk], vf);
-                        if (h2 * 32 + i * 16 + n >= here) vf[x] = __builtin_bit_cast(bf16x8_t, make_uint4(0u, 0u, 0u, 0u));
-                        *reinterpret_cast<bf16x8_t *>(put[kk] + i * 16 * 2 * D) = vf[x];
+                        typename Terms<T>::Raw raw;
+                        bf16x8_t kf[NQ];
+                        if constexpr (APART) __builtin_amdgcn_sched_barrier(0);      // (or the loads of all pieces take registers)
+                        Terms<T>::load(Kc + (size_t)min(ch * 64 + kt * 16 + n, kept - 1) * D + gr * (D / 4) + kk * 8, raw);
+                        bf16x8_t far;
+                        if constexpr (APART) far = Terms<T>::take_infinite(raw);
+                        Terms<T>::cut(raw, kf);
+#pragma unroll
+                        for (int u = 0; u < QT; ++u)
+#pragma unroll
+                            for (int x = NQ - 1; x >= 0; --x)
+#pragma unroll
+                                for (int y = NQ - 1 - x; y >= 0; --y) st[u][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x], qf[u][kk][y], st[u][kt], 0, 0, 0);
+                        if constexpr (APART) {
+#pragma unroll
+                            for (int u = 0; u < QT; ++u) st[u][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(far, qf[u][kk][0], st[u][kt], 0, 0, 0);
+                        }
                     }
-                values(pb, h2, x);
+                }
+#pragma unroll
+                for (int u = 0; u < QT; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (kt * 16 + 4 * gr + e >= here) st[u][kt][e] = -INFINITY;
             }
+#pragma unroll
+            for (int u = 0; u < QT; ++u) soft(u, st[u], pb[u]);
+#pragma unroll
+            for (int h2 = 0; h2 < 2; ++h2) {
+                if (NQ > 1 && h2 * 32 >= here) break;
+                typename Terms<T>::Raw raw[2][KS];
+                auto load = [&](int i, int kk) __attribute__((always_inline)) {
+                    Terms<T>::load(Vc + (size_t)min(ch * 64 + h2 * 32 + i * 16 + n, kept - 1) * D + gr * (D / 4) + kk * 8, raw[i][kk]);
+                };
+                if (NQ > 1 && !APART) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int kk = 0; kk < KS; ++kk) load(i, kk);
+                }
+#pragma unroll
+                for (int x = NQ - 1; x >= 0; --x) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int kk = 0; kk < KS; ++kk) {
+                            bf16x8_t vf[NQ];
+                            if constexpr (APART) __builtin_amdgcn_sched_barrier(0);
+                            if (NQ == 1 || APART) load(i, kk);
+                            if constexpr (APART) Terms<T>::take_infinite(raw[i][kk]);
+                            Terms<T>::cut(raw[i][kk], vf);
+                            if (h2 * 32 + i * 16 + n >= here) vf[x] = __builtin_bit_cast(bf16x8_t, make_uint4(0u, 0u, 0u, 0u));
+                            *reinterpret_cast<bf16x8_t *>(put[kk] + i * 16 * 2 * D) = vf[x];
+                        }
+                    values(pb, h2, x);
+                }
+                if constexpr (APART) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int kk = 0; kk < KS; ++kk) {
+                            __builtin_amdgcn_sched_barrier(0);
+                            load(i, kk);
+                            bf16x8_t far = Terms<T>::take_infinite(raw[i][kk]);
+                            if (h2 * 32 + i * 16 + n >= here) far = __builtin_bit_cast(bf16x8_t, make_uint4(0u, 0u, 0u, 0u));
+                            *reinterpret_cast<bf16x8_t *>(put[kk] + i * 16 * 2 * D) = far;
+                        }
+                    values(pb, h2, NP - 1);
+                }
+            }
+        }
+    };
+    store_rows(std::false_type{});
+    if (c0 + wave < min(sc, c1)) {
+        float sum = 0.f;                         // (NaN if one of them is, or two are infinite)
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            sum += lsum[u];
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) sum += (o[u][dt][0] + o[u][dt][1]) + (o[u][dt][2] + o[u][dt][3]);
+        }
+        if (__any(sum != sum)) {                 // (rare)
+            reset();
+            store_rows(std::true_type{});
         }
     }
 
