@@ -350,9 +350,10 @@ int kvev_page_read(const kvev_shape *shape, const kvev_pages *pages, const void 
  * Else query i is token q_start[b] + i and sees those up to itself; with q_start as
  * kvev_pages_reserve gives it, the queries are the tokens just appended.  (In a padded batch,
  * queries from n_new[b] on get an output that means nothing, and so do those of a row whose start
- * is -1.)  Tokens without a page are left out.  A query that sees no row, or whose scores are all
- * minus infinity, gives zeros.  Summaries that are infinite act as the formula has them: such a
- * value reaches its element of every query with its sign (NaN where its fp32 weight is 0).
+ * is -1.)  Tokens without a page are left out.  A query that sees no row gives zeros, and
+ * so does one whose elements are finite and whose scores are all minus infinity.  Summaries that
+ * are infinite act as the formula has them: such a value reaches its element of every query with
+ * its sign (NaN where its fp32 weight is 0).
  * Scores, softmax and sums are fp32, O is rounded once.  fp32: operands enter the matrix cores as
  * three bf16 terms; bf16: the softmax weights as two, 16 significant bits, or as one rounded to
  * bf16 in frames (48 queries or more to a key-value head, and enough rows to pay for the form),

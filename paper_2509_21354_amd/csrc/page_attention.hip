@@ -20,8 +20,8 @@
 // ends of rows, the join); 32 heads x 4091 tokens 11 us (launch and a chain of five round trips: length and table, codes, partials,
 // ticket, partials again).  Four waves on a SIMD spill (629 us).  Tried and dropped, no gain: prefetching without branches, a peeled last
 // chunk, store rows asked for ahead; equal shares of all chunks for as many workgroups as fit (410).
-// fp32: the queries enter as three bf16 terms of 8 bits, the weights likewise, rows of the store too (products of terms below
-// 2^-24 left out).  bf16: the weights enter as two terms.
+// fp32: the queries enter as three bf16 terms of 8 bits, the weights likewise, rows of the store too (of the products of terms those
+// are left out that come to 2^-24 of the whole product, see cut3).  bf16: the weights enter as two terms.
 //
 // Values that are not finite: a block of the cache that held one has the scale byte 255 and reads as NaN.  Such keys make their
 // token's scores NaN, which a query that must not see the token replaces.  Values would reach every query of the tile as 0 * NaN,
@@ -42,27 +42,24 @@ namespace kvev {
 __device__ __forceinline__ void store_device(float *p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ float load_device(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// fp32 values cut into three bf16 terms of 8 significant bits each (their sum is the value)
+// fp32 values as three bf16 terms, each the rounded rest of those before: their sum is the value.  The rest of a value of
+// magnitude 1 to 2 is below 2^-8 behind the first term and at most 2^-17 behind the second, so of a product of two such values the terms that
+// are left out (second times third, third times third) come to less than 2^-24 (1 + 2^-9), with either sign.  (Terms cut off instead
+// of rounded have the value's sign: what was left out added up, to as much as 2^-21.)  A value that is not finite has NaN among its terms.
 __device__ __forceinline__ void cut3(const float (&x)[8], bf16x8_t (&t)[3])
 {
+    const float most = __uint_as_float(0x7F7F7FFFu);             // rounded to bf16 the values above would be infinite
     uint32_t w[3][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        uint32_t c[3][2];
+        w[0][i] = pack_bf16x2(__builtin_amdgcn_fmed3f(x[2 * i], -most, most), __builtin_amdgcn_fmed3f(x[2 * i + 1], -most, most));
+        float r[2] = {x[2 * i], x[2 * i + 1]};
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const float v = x[2 * i + e];
-            const uint32_t h = __float_as_uint(v) & 0xFFFF0000u;
-            const bool finite = (h & kInfBits) != kInfBits;
-            const float r = finite ? v - __uint_as_float(h) : 0.f;
-            const uint32_t m = __float_as_uint(r) & 0xFFFF0000u;
-            // (a NaN whose payload sits in the low half stays one)
-            c[0][e] = (finite ? h : __float_as_uint(v + v) ) >> 16;
-            c[1][e] = m >> 16;
-            c[2][e] = __float_as_uint(r - __uint_as_float(m)) >> 16;
+        for (int k = 1; k < 3; ++k) {
+            r[0] -= __uint_as_float(w[k - 1][i] << 16);
+            r[1] -= __uint_as_float(w[k - 1][i] & 0xFFFF0000u);
+            w[k][i] = pack_bf16x2(r[0], r[1]);
         }
-#pragma unroll
-        for (int k = 0; k < 3; ++k) w[k][i] = c[k][0] | c[k][1] << 16;
     }
 #pragma unroll
     for (int k = 0; k < 3; ++k) t[k] = __builtin_bit_cast(bf16x8_t, make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]));
@@ -114,16 +111,17 @@ template <> struct Terms<float> {
     static __device__ __forceinline__ void cut(const Raw &r, bf16x8_t (&t)[3]) { cut3(r.v, t); }
     static __device__ __forceinline__ bf16x8_t take_infinite(Raw &r)
     {
-        Raw far;
-        bf16x8_t t[3];
+        float far[8];
+        uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const bool finite = (__float_as_uint(r.v[e]) & kInfBits) != kInfBits;
-            far.v[e] = finite ? 0.f : r.v[e];
-            if (!finite) r.v[e] = 0.f;
+            far[e] = finite ? 0.f : r.v[e];
+            r.v[e] = finite ? r.v[e] : 0.f;
         }
-        cut3(far.v, t);
-        return t[0];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(far[2 * i], far[2 * i + 1]);
+        return __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
     }
 };
 

@@ -1,4 +1,5 @@
-"""Values of a paged cache and of the kept summaries beside it that are out of the ordinary."""
+"""Values of a paged cache and of the kept summaries beside it that are out of the ordinary: infinities, mantissas that are hard to
+cut into terms, the largest numbers."""
 import numpy as np
 import pytest
 import torch
@@ -83,3 +84,45 @@ def test_query_whose_scores_are_all_minus_infinity(dtype, Tq, frames):
     O = torch.full_like(Q, 9.0)
     c.attend(Q, Tq, O, Kc=Kc, Vc=Vc, count=ints([[[5], [0]]]), k_cap=5)
     assert (O == 0).all()
+
+
+def test_fp32_summaries_whose_terms_are_hard_to_cut():
+    """Two summaries with one element each, whose scores of 2^16 differ by less than 1: keys that bf16 terms of full size make up, and
+    bf16 keys beside them.  One product has three roundings in fp32 at most (a sum of the terms rounds at its last step, by a unit of 2^-24 or, cut
+    off, two; products that are left out come to one), the other key's two; scaling and the difference are rounded at its own size."""
+    B, Tq, d = 64, 16, 64
+    sh = shape_of(1, B, 1, 1, d, torch.float32)
+    c = kb.PagedCache(sh, 16, 1, 1, Tq)
+    rng = np.random.default_rng(5)
+    low = np.where(np.arange(B) % 2, 0xFFFF, rng.integers(0xFF00, 0x10000, B))
+    kA = ((0x3F800000 | (rng.integers(0, 0x80, B) << 16) | low).astype(np.uint32)).view(np.float32)
+    kB = torch.from_numpy(kA).bfloat16().float().numpy()
+    q = ((0x3F800000 | (rng.integers(0, 0x80, (B, Tq)) << 16) | np.where(np.arange(Tq) % 2, 0xFFFF, rng.integers(0, 0x10000, (B, Tq)))).astype(np.uint32)).view(np.float32)
+    kA[0], kB[0], q[0, 0] = np.uint32(0x3F80FFFF).view(np.float32), 1.0078125, np.uint32(0x3F80FFFF).view(np.float32)
+    assert (np.abs(kA.astype(np.float64) - kB) <= 2.0 ** -15).all()
+    Kc, Vc, Q = torch.zeros(1, B, 1, 2, d), torch.zeros(1, B, 1, 2, d), torch.zeros(1, B, 1, Tq, d)
+    Kc[0, :, 0, 0, 0], Kc[0, :, 0, 1, 0] = torch.from_numpy(kA) * 2 ** 9, torch.from_numpy(kB) * 2 ** 9
+    Vc[..., 0, 0], Vc[..., 1, 0] = 1, -1
+    Q[0, :, 0, :, 0] = torch.from_numpy(q) * 2 ** 10
+    O = torch.empty_like(Q, device="cuda")
+    kb.kvev_page_attention(sh, c.pages, Q.cuda(), Tq, c.pool, c.table, c.length, O, c.ws_attn, Kc=Kc.cuda(), Vc=Vc.cuda(),
+                           count=torch.full((1, B, 1), 2, dtype=I32, device="cuda"), k_cap=2)
+    a, b = (q.astype(np.float64) * k[:, None] * 2.0 ** 19 / 8 for k in (kA.astype(np.float64), kB.astype(np.float64)))
+    err = np.abs(O[0, :, 0, :, 0].cpu().double().numpy() - np.tanh((a - b) / 2))
+    # the weights' difference moves by half of the scores'; its own roundings, exp2's and the division's are a few units
+    print("largest error, in units of 2^-24 of the score:", float((err / (a * 2.0 ** -25)).max()))
+    assert (err <= 5 * 2.0 ** -24 * a / 2 + 16 * 2.0 ** -24).all(), float((err / (a * 2.0 ** -25)).max())
+
+
+def test_fp32_summaries_of_the_largest_values():
+    """Rounded to bf16 they would be infinite.  One row, weight 1: its values come out, off by the output's rounding and the products' two."""
+    sh = shape_of(1, 1, 1, 1, 64, torch.float32)
+    c = kb.PagedCache(sh, 16, 1, 1)
+    top = torch.tensor([0x7F7FFFFF, 0x7F7F8000, 0x7F7F7FFF, 0x7F7F8001]).to(I32).view(torch.float32)
+    Kc, Vc, Q = torch.zeros(1, 1, 1, 1, 64), torch.zeros(1, 1, 1, 1, 64), torch.zeros(1, 1, 1, 1, 64)
+    Kc[..., :4], Q[..., :4] = top, 2.0 ** -100
+    Vc[..., :4], Vc[..., 60:] = top, -top
+    O = torch.full_like(Q, 9.0, device="cuda")
+    Q[..., 8:12] = top
+    c.attend(Q.cuda(), 1, O, Kc=Kc.cuda(), Vc=Vc.cuda(), count=ints([[[1]]]), k_cap=1)
+    assert ((O.cpu().double() - Vc.double()).abs() <= 3 * 2.0 ** -24 * Vc.double().abs()).all()
