@@ -331,8 +331,9 @@ size_t kvev_page_workspace_bytes(int op, const kvev_shape *shape, const kvev_pag
  * start[b] + t (n_new NULL: all Tn; more than Tn count as Tn; L * B * H_kv * Tn <= 2^30).
  * Nothing is written for a batch row with start[b] < 0, nor for tokens past the capacity or
  * without a page.  Tokens that are there may be written again.  No two rows of a call may name
- * the same token of the same page.  Does not look at lengths: kvev_pages_reserve makes room,
- * moves them on and gives `start`. */
+ * the same token of the same page.  Does not look at lengths or holders (what goes into a page that
+ * several batch rows hold is there for all of them): kvev_pages_reserve makes room, gives a row a
+ * page of its own, moves lengths on and gives `start`. */
 int kvev_page_append(const kvev_shape *shape, const kvev_pages *pages, const void *K, const void *V, int Tn,
                      const int32_t *start, const int32_t *n_new, const int32_t *table, void *pool, void *stream);
 

@@ -573,16 +573,19 @@ class PagedCache:
         self.pool = torch.empty(nbytes, dtype=torch.uint8, device=device)
         self.table, self.length, self.refs = ints(shape.B, max_pages, fill=-1), ints(shape.B), ints(n_pages)
         self.start, self.status = ints(shape.B), ints(1)
+        self.n_new = None                        # the counts of the last reserve()
         self.ws = alloc_workspace(page_workspace_bytes(OP_PAGES_RESERVE, shape, self.pages, 0), device)
         # (the attention's own: its tickets must stay zero between calls)
         self.ws_attn = alloc_workspace(page_workspace_bytes(OP_PAGE_ATTENTION, shape, self.pages, Tq), device)
 
     def reserve(self, n_new):
         kvev_pages_reserve(self.shape, self.pages, n_new, self.table, self.length, self.refs, self.pool, self.start, self.status, self.ws)
+        self.n_new = n_new
 
     def append(self, K, V, Tn, n_new=None):
-        """The rows for which reserve() last made room."""
-        kvev_page_append(self.shape, self.pages, K, V, Tn, self.start, n_new, self.table, self.pool)
+        """The rows for which reserve() last made room, from `start` on: n_new of each batch row, or as many as reserve() was given
+        (its tensor is read once more, when the rows are written).  All Tn of each before the first reserve()."""
+        kvev_page_append(self.shape, self.pages, K, V, Tn, self.start, self.n_new if n_new is None else n_new, self.table, self.pool)
 
     def attend(self, Q, Tq, O, first=None, causal=False, Kc=None, Vc=None, count=None, k_cap=0):
         """causal: the queries are the tokens for which reserve() last made room."""
