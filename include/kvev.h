@@ -363,7 +363,8 @@ int kvev_page_read(const kvev_shape *shape, const kvev_pages *pages, const void 
  * in the order of sums and the choice of the form only.
  * Workspace: kvev_page_workspace_bytes(KVEV_OP_PAGE_ATTENTION, shape, pages, Tq), enough for every
  * T and for fewer queries; zero-filled before its first use, tickets as in kvev_gated_attention.
- * Calls of any Tq and T may take the same one, one after the other.  O must not overlap Q. */
+ * Calls of any Tq and T may take the same one, one after the other.  O must not overlap Q.  Needs
+ * L * B * H * Tq <= 2^26 and L * B * H_kv * k_cap < 2^31. */
 int kvev_page_attention(const kvev_shape *shape, const kvev_pages *pages, const void *Q, int Tq, const void *pool,
                         const int32_t *table, const int32_t *length, const int32_t *first, const int32_t *q_start,
                         const void *Kc, const void *Vc, const int32_t *count, int k_cap, void *O, void *ws,

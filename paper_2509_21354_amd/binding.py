@@ -32,6 +32,7 @@ OP_CHUNK_POOL, OP_LSTM_GATE, OP_SELECT, OP_GATED_ATTENTION, OP_DENSE_ATTENTION, 
 OP_LSTM_PREPARE, OP_LSTM_GATE_PREPARED = 6, 7
 OP_PAGE_ATTENTION, OP_PAGES_RESERVE, OP_PAGES_COMPACT = 16, 17, 18
 PAGES_NONE_FREE, PAGES_BAD_ROW, PAGES_BAD_PAIR = 1, 2, 4          # bits of a paged cache's status word
+PAGE_QUERIES = 1 << 26                                            # L * B * H * Tq of kvev_page_attention, at most
 ROTARY_HALVES, ROTARY_PAIRS = 0, 1
 
 EXPORTS = ("kvev_chunk_pool", "kvev_lstm_gate", "kvev_lstm_prepare", "kvev_lstm_gate_prepared", "kvev_select", "kvev_gated_attention",
@@ -567,6 +568,8 @@ class PagedCache:
         nbytes = page_pool_bytes(shape, self.pages)
         if nbytes == 0:
             raise KvevError(ERR_INVALID_ARG, f"no such cache: pages of {page} tokens, {n_pages} of them, {max_pages} to a row")
+        if not 0 <= Tq <= PAGE_QUERIES // (shape.L * shape.B * shape.H):
+            raise KvevError(ERR_INVALID_ARG, f"a cache attends to no more than {PAGE_QUERIES} queries of all layers, rows and heads, not to {Tq} of each")
 
         def ints(*size, fill=0):
             return torch.full(size, fill, dtype=torch.int32, device=device)
