@@ -422,7 +422,8 @@ int kvev_pages_compact(const kvev_shape *shape, const kvev_pages *pages, const v
  * Q, K the gradients of the outputs, the outputs are those of the inputs.
  *   Q, Q_out [L,B,H,Tq,d], K, K_out [L,B,H_kv,Tq,d]  (either pair may be NULL; in place: the same
  *   pointer, else no two may overlap)      freq [P] fp32      pos [n_axes,B,Tq] int32
- * Angles are taken in 64 bits, products in fp32, each element is rounded once.  Needs
+ * Angles are taken and reduced in 64 bits, and what is left of a turn is rounded to fp32 (by 2^-26 of
+ * a turn at most); sine, cosine and products are fp32, each element is rounded once.  Needs
  * 1 <= P <= d / 2, sections >= 0, L * B * H * Tq <= 2^28. */
 typedef struct { int32_t n_axes, section[4], layout; } kvev_rotary_axes;
 enum { KVEV_ROTARY_HALVES = 0, KVEV_ROTARY_PAIRS = 1 };

@@ -15,8 +15,8 @@
 // that share a unit's rows meet in scratch (partials, a ticket, the last one to arrive merges in split order).  A unit has one or
 // two such tiles of 16 queries (QT): with two, converting and staging a row is paid once for both (512 heads x 32 queries x 4000
 // tokens 110 and 73 us).
-// What bounds it (d = 128, bf16): 32 layers x 8 rows x 8 heads x 8192 tokens, 2.29 GB, 365 - 374 us = 6.1 - 6.3 TB/s with the vector unit 54 %
-// and the matrix cores 27 % busy, a reader without arithmetic reaches 7.2; 64 x 8 heads of ragged rows up to 8192 61 us = 4.8 TB/s (the
+// What bounds it (d = 128, bf16): 32 layers x 8 rows x 8 heads x 8192 tokens, 2.29 GB, 358 - 378 us = 6.0 - 6.4 TB/s with the vector unit 51 %
+// and the matrix cores 26 % busy, a reader without arithmetic reaches 7.2; 64 x 8 heads of ragged rows up to 8192 60 - 63 us = 4.6 - 4.8 TB/s (the
 // ends of rows, the join); 32 heads x 4091 tokens 11 us (launch and a chain of five round trips: length and table, codes, partials,
 // ticket, partials again).  Four waves on a SIMD spill (629 us).  Tried and dropped, no gain: prefetching without branches, a peeled last
 // chunk, store rows asked for ahead; equal shares of all chunks for as many workgroups as fit (410).
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW < 8 && QT == 1 ? 3 : 
 
     // ---- rows of the store ----
     // (fp32: cutting a row into terms is most of the work, so half chunks without rows are passed over and values are read once for all
-    // terms: 16 summaries of 2 x 4 heads x 33 queries add 0.4 us to 6.8, 3.5 without)
+    // terms: 16 summaries of 2 x 4 heads x 33 queries and 320 tokens take 6.6 us, as do the tokens alone; they added 3.5 without)
     // (APART: what is not finite by itself)
     int ch;
     auto store_rows = [&](auto apart) __attribute__((always_inline)) {

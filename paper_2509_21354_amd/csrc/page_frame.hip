@@ -9,8 +9,8 @@
 // the transposing LDS load; weights of a step made under the products of the one before.
 // The weights enter the second product rounded to bf16 (the output is rounded to no more bits, and their terms' second half would cost as
 // many matrix instructions again); the normaliser sums the rounded ones, two to an instruction.
-// Measured (d = 128): 16 rows x 8 heads x 1024 queries over 8192 tokens, 541 GFLOP, 519 us = 1042 TFLOP/s, where the library's bf16
-// product of 8192^3 reaches 1231.  Matrix and vector work take about as many clocks of a SIMD and hardly overlap: that bounds it.
+// Measured (d = 128): 16 rows x 8 heads x 1024 queries over 8192 tokens, 541 GFLOP, 511 - 552 us = 980 - 1058 TFLOP/s, where the library's bf16
+// product of 8192^3 reaches 1231.  Matrix and vector work take 45 % of a SIMD's clocks each and hardly overlap: that bounds it.
 // Tried and dropped: raised wave priority around the products (no difference); half of the waves staging behind their products (553 for
 // 527 us); the two waves of a SIMD half a tile apart, one making scores while the other makes weights (611 for 541); the next
 // tile converted between the products (533 for 519).

@@ -4,8 +4,9 @@
 // order.  Whoever needs pages takes the free ones of lowest index, in the order of the rows, so a call's outcome depends on
 // nothing but what the arrays held before it.  Atomics are integer additions and exchanges whose order does not show.
 // Tables and counts are small (a few bytes per page): those kernels are chains of memory round trips, one workgroup each where
-// they have to see all rows (16 rows, 560 pages: reserve 6.2 us, its copies 6.6, fork 4.3, trim 4.1; compaction's ranks of 5 200 pages 8).  Copies
-// move whole 16-byte pieces at the rate of the memory (compaction of 1.7 GB in and out: 318 us, 5.4 TB/s; a large copy: 4.9).
+// they have to see all rows (16 rows, 560 pages: reserve 6.1 us, its copies 6.5, fork 3.9, trim 3.9; compaction's ranks of 5 200 pages 8.7).  Copies
+// move whole 16-byte pieces at the rate of the memory (compaction of 1.7 GB in and out: 322 us, 5.3 TB/s; copies of 512 pages of 32 layers, 2.3
+// GB in and out, 455 us, 5.0, of 8192 pages of one layer 242 us, 4.7; a large copy: 4.9).
 #include "kernels.hpp"
 #include "pages.hpp"
 
