@@ -339,7 +339,8 @@ int kvev_page_append(const kvev_shape *shape, const kvev_pages *pages, const voi
 
 /* Rows out of the pages, exactly (for kvev_chunk_pool, which takes contiguous rows): token
  * first[b] + t goes to row t < n[b] of K, V [L,B,H_kv,Tn,d] (n NULL: all Tn); zeros where
- * there is no page.  Rows from n[b] on are left as they were, and so is everything of a batch
+ * there is no page (lengths are not looked at: what lies behind one is whatever the page holds).
+ * Rows from n[b] on are left as they were, and so is everything of a batch
  * row with first[b] < 0 and what lies past the capacity. */
 int kvev_page_read(const kvev_shape *shape, const kvev_pages *pages, const void *pool, const int32_t *table,
                    const int32_t *first, const int32_t *n, int Tn, void *K, void *V, void *stream);
@@ -358,7 +359,8 @@ int kvev_page_read(const kvev_shape *shape, const kvev_pages *pages, const void 
  * Scores, softmax and sums are fp32, O is rounded once.  fp32: operands enter the matrix cores as
  * three bf16 terms; bf16: the softmax weights as two, 16 significant bits, or as one rounded to
  * bf16 in frames (48 queries or more to a key-value head, and enough rows to pay for the form),
- * whose normaliser sums the rounded ones.  shape->T (0: the capacity)
+ * whose normaliser sums the rounded ones.  Values are summed under weights of up to 2^8 before the
+ * division by the weights' sum: n rows of magnitudes from 2^120 / n on may leave fp32.  shape->T (0: the capacity)
  * says for what length of row the launch is made; any length is right, and results depend on it
  * in the order of sums and the choice of the form only.
  * Workspace: kvev_page_workspace_bytes(KVEV_OP_PAGE_ATTENTION, shape, pages, Tq), enough for every
