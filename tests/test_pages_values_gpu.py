@@ -126,3 +126,20 @@ def test_fp32_summaries_of_the_largest_values():
     Q[..., 8:12] = top
     c.attend(Q.cuda(), 1, O, Kc=Kc.cuda(), Vc=Vc.cuda(), count=ints([[[1]]]), k_cap=1)
     assert ((O.cpu().double() - Vc.double()).abs() <= 3 * 2.0 ** -24 * Vc.double().abs()).all()
+
+
+@pytest.mark.parametrize("dtype,Tq,kept", [(torch.float32, 3, 0), (torch.float32, 20, 40), (torch.bfloat16, 3, 40), (torch.bfloat16, 60, 40)])
+def test_queries_that_are_not_finite_keep_to_themselves(dtype, Tq, kept, frames):
+    sh = shape_of(1, 2, 4, 2, 64, dtype)
+    c = cache_of(sh, 16, [130, 130], Tq=Tq)
+    fill(c, [130, 130], dtype)
+    Q = normal(7, 1, 2, 4, Tq, 64, dtype=dtype)
+    store = (normal(8, 1, 2, 2, 40, 64, dtype=dtype), normal(9, 1, 2, 2, 40, 64, dtype=dtype), torch.full((1, 2, 2), kept, dtype=I32, device="cuda"))
+    O, P = torch.empty_like(Q), torch.empty_like(Q)
+    c.attend(Q, Tq, O, None, False, *store, 40)
+    bad = Q.clone()
+    bad[0, 0, 1, 1, 5], bad[0, 1, 2, 0, 0], bad[0, 1, 3, Tq - 1, 63] = NAN, INF, -INF
+    c.attend(bad, Tq, P, None, False, *store, 40)
+    hit = torch.zeros(1, 2, 4, Tq, dtype=torch.bool, device="cuda")
+    hit[0, 0, 1, 1] = hit[0, 1, 2, 0] = hit[0, 1, 3, Tq - 1] = True
+    assert torch.isnan(P[hit]).all() and torch.equal(P[~hit], O[~hit]) and torch.isfinite(O).all()
